@@ -294,6 +294,138 @@ int elm_stream_cache(const elm_stream *s, const elm_params *params, int32_t *idx
                      int32_t *count_host, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Rotary positions.  Number pairs (a, b) of a head's first rotary_dim numbers turn by angle position * inv_freq[i]:
+ *   a' = a c - b s,  b' = b c + a s,  c = scale cos(angle), s = scale sin(angle);
+ * pair i is (i, i + rotary_dim / 2) with ELM_ROPE_HALVES and (2 i, 2 i + 1) with ELM_ROPE_PAIRS; the numbers from
+ * rotary_dim on are copied.  `inverse` negates s: the gradient of the rotation (its transpose), and with scale = 1 the
+ * rotation back.  Angles are reduced exactly (64-bit fractions of a turn), cosines and sines formed in fp64 and rounded to
+ * fp32, products and sums in fp32, one rounding to the storage type.
+ */
+enum { ELM_ROPE_HALVES = 0, ELM_ROPE_PAIRS = 1 };
+typedef struct elm_rope_params {
+    int32_t batch, heads, n_tokens, d;  /* d: 2 .. 256, even */
+    int32_t dtype;                      /* ELM_F32 or ELM_BF16, of X and out */
+    int32_t rotary_dim;                 /* even, 2 .. d */
+    int32_t layout;                     /* ELM_ROPE_HALVES or ELM_ROPE_PAIRS */
+    int32_t inverse;
+    double scale;                       /* factor on the rotated numbers; finite */
+    const double *inv_freq;             /* HOST array[rotary_dim / 2], radians per position; finite; read during the call */
+    int64_t x_stride[3], out_stride[3]; /* batch, head, token strides in elements (the numbers of a head lie side by
+                                           side); all three 0: dense [batch][heads][n_tokens][d] */
+} elm_rope_params;
+/* X, out: any element-aligned addresses and strides (16-byte aligned rows are faster); out may be X with the same strides,
+ * else the two must not overlap, and no two rows of out may.  positions: device int32 [batch][n_tokens], any sign; NULL:
+ * token t of every batch entry has position first_position + t. */
+int elm_rope(const void *X, const int32_t *positions, int64_t first_position, const elm_rope_params *params, void *out,
+             void *stream);
+/* Frequencies base^(-2 i / rotary_dim) and their forms for contexts longer than the trained length `original`:
+ *   PLAIN   as they are
+ *   LINEAR  divided by factor
+ *   BASE    base multiplied by factor^(rotary_dim / (rotary_dim - 2)), so that the slowest pair is divided by factor
+ *   RAMP    a blend of PLAIN and LINEAR by the pair's number: PLAIN up to the pair that makes `high` turns over `original`
+ *           positions, LINEAR from the one that makes `low`, linear between; *scale = 0.1 ln(factor) + 1 (factor > 1)
+ *   SMOOTH  the blend by the pair's turns t over `original`: share of PLAIN = (t - low) / (high - low) within [0, 1]
+ * inv_freq_host [rotary_dim / 2] and scale_host receive the result (HOST). */
+enum { ELM_ROPE_PLAIN = 0, ELM_ROPE_LINEAR = 1, ELM_ROPE_BASE = 2, ELM_ROPE_RAMP = 3, ELM_ROPE_SMOOTH = 4 };
+int elm_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double original, double low,
+                         double high, double *inv_freq_host, double *scale_host);
+
+/*
+ * Rows held in 4 bits, in pages.  A row holds the key and the value of one token and KV head: d / 2 bytes of the key's codes
+ * (number 2 j in the low half of byte j), d / 2 of the value's, d / 16 scales of the key, d / 16 of the value; d = 128: 144
+ * bytes, d = 64: 72 and 8 unused ones (elm_cache4_row_bytes).  A code is an E2M1 number (sign, magnitude 0, 1/2, 1, 3/2, 2, 3, 4 or 6); each
+ * stretch of 16 numbers has a scale of 8 bits, the upper byte-and-a-bit of an fp16 number (sign left out: 5 exponent bits,
+ * 3 mantissa bits), and a number is code x scale, exact in bf16.  Storing rounds the largest magnitude of the stretch over 6 to a
+ * scale (nearest, ties to even; at most 10240: numbers beyond +-61440 become that) and each number over the scale to a code
+ * (nearest, ties to even).  A stretch with a NaN is stored as NaN.
+ * The pool is rows[n_pages][kv_heads][page_rows][row bytes], 16-byte aligned, page_rows a power of two from 16 to 1024.  Row r of a
+ * request is row r % page_rows of page table[request][r / page_rows]; a table is device int32 [batch][max_pages].  Numbers
+ * outside [0, n_pages) are no pages: nothing is read or written through them.  A slot is page * page_rows + row in page, an
+ * int32; n_pages * page_rows must not exceed 2^31 - 1, kv_heads times that 2^32 - 1.
+ */
+int elm_cache4_row_bytes(int32_t d, size_t *bytes);
+
+/* Pages, positions and slots of a step's new tokens, from device lengths alone (no synchronisation; capturable).  Request b has
+ * length[b] rows in its pages (table entries up to ceil(length / page_rows)) and n_new[b] tokens coming, which lie one
+ * request after the other among the step's max_tokens places (a step may be padded).  Requests are served in order: a request gets its
+ * pages from the end of the list free[0 .. *free_count), or, where it does not fit (the table's max_pages, max_tokens, or more
+ * pages wanted by the requests up to it than are free; a negative length or n_new) is left as it was, with its tokens' places
+ * marked.  A request that wants no page is never short of one.
+ *   table        entries of new pages are written, nothing else
+ *   start_out    [batch] first position of the new tokens (= length), or -1 for a request that did not fit
+ *   length_out   [batch] rows after the step; may be `length` itself
+ *   free_count_out  [1]; may be `free_count` itself.  free is not written: entries past the new count are the taken ones
+ *   cu_out       [batch + 1] first place of each request's tokens, and their total (negative n_new count as 0)
+ *   position_out, slot_out  [max_tokens] of every place; -1 where there is no token or its request did not fit
+ * batch 1 .. 65536; max_tokens >= 0; free_count above the list's capacity n_free counts as n_free. */
+typedef struct elm_page_params {
+    int32_t batch, max_pages, page_rows, max_tokens, n_free;
+} elm_page_params;
+int elm_page_plan(int32_t *table, const int32_t *length, const int32_t *n_new, const int32_t *free, const int32_t *free_count,
+                  const elm_page_params *params, int32_t *start_out, int32_t *length_out, int32_t *free_count_out,
+                  int32_t *cu_out, int32_t *position_out, int32_t *slot_out, void *stream);
+/* Gives the pages of every request with done[b] != 0 back: they are put at the end of free (in order of request and page), its table
+ * entries become -1, its length 0.  *free_count is updated; pages for which free (capacity n_free) has no room, and table entries that
+ * are negative, are dropped.  max_tokens is not used. */
+int elm_page_release(int32_t *table, int32_t *length, const int32_t *done, int32_t *free, int32_t *free_count,
+                     const elm_page_params *params, void *stream);
+
+/* New tokens into the pool: keys are rotated, keys and values stored in 4 bits; queries, if any, rotated beside them.
+ *   K, V [n_tokens][kv_heads][d], Q and Q_out [n_tokens][q_heads][d] (Q_out may be Q), with token and head strides in elements
+ *   (both 0: dense).  positions int32 [n_tokens] (unused when rotary_dim is 0), slots int32 [n_tokens]: a token whose slot is outside the pool
+ *   is passed over: neither its row nor its Q_out is written.  Two tokens must not have the same slot. */
+typedef struct elm_append_params {
+    int32_t n_tokens, q_heads, kv_heads, d; /* q_heads 0: no queries; d 64 or 128 */
+    int32_t dtype;                          /* ELM_F32 or ELM_BF16, of Q, K, V and Q_out */
+    int32_t page_rows, n_pages;
+    int32_t rotary_dim, layout;             /* rotary_dim 0: nothing is rotated */
+    double scale;
+    const double *inv_freq;                 /* HOST, as in elm_rope_params */
+    int64_t q_stride[2], k_stride[2], v_stride[2], q_out_stride[2];
+} elm_append_params;
+int elm_cache4_append(const void *Q, const void *K, const void *V, const int32_t *positions, const int32_t *slots,
+                      const elm_append_params *params, void *Q_out, void *rows, void *stream);
+
+/* Rows back: K_out, V_out dense [batch][kv_heads][n_kv][d] in dtype (ELM_F32 or ELM_BF16, exact either way), as elm_compress and
+ * elm_express_prefill take them.  idx NULL: row r of request b is its row r; else idx[batch][kv_heads][n_kv] are the rows' numbers
+ * (those of elm_compress, say).  A row that is not there (r < 0, r >= length[b] where length is given, past the table, on no
+ * page) reads as zeros. */
+typedef struct elm_cache4_params {
+    int32_t batch, q_heads, kv_heads, d;    /* d 64 or 128; q_heads is not used by elm_cache4_read */
+    int32_t dtype;
+    int32_t page_rows, n_pages, max_pages;
+    int32_t n_kv;                           /* read: rows per request; attend: list entries, or an upper bound of the lengths
+                                               (0: max_pages * page_rows) */
+    int32_t n_q;                            /* attend: query rows per request; with cu the most of any request */
+    int32_t n_tokens;                       /* attend with cu: tokens that Q and O hold */
+    int32_t causal;                         /* attend over lengths: query j of n sees the first length - n + 1 + j rows */
+    int64_t q_stride[3], o_stride[3];       /* attend: batch, head, token strides in elements; all 0: dense
+                                               [batch][q_heads][n_q][d], with cu [n_tokens][q_heads][d] */
+} elm_cache4_params;
+int elm_cache4_read(const void *rows, const int32_t *table, const int32_t *length, const int32_t *idx,
+                    const elm_cache4_params *params, void *K_out, void *V_out, void *stream);
+
+/*
+ * Eq. (def:att_approx) over rows held in 4 bits.  Exactly one of `length` and `idx` is given:
+ *   length [batch]       the request's rows 0 .. length - 1 (the exact attention of Eq. (unmaskedatt); with `causal` of its last n_q tokens,
+ *                        Eq. (def:att)).  Requests with different numbers of queries: cu [batch + 1] on the device (that of
+ *                        elm_page_plan), request b has the tokens cu[b] .. cu[b + 1] - 1 of Q and O; batch strides are not used.
+ *   idx, w [batch][kv_heads][n_kv]  a weighted list of the request's rows, as elm_attend takes it; every query sees all of it.
+ * Rows that are not there, and list entries whose weight is not above 0, are not seen, whatever they hold; a query that sees
+ * nothing gets zeros.  Tokens of O outside cu, and those of requests without queries, are left as they were.
+ * dtype is that of Q and O: ELM_BF16 (probabilities rounded to fp16 for P V) or ELM_F32 (queries and probabilities as two fp16
+ * parts); logits, maxima, denominators and accumulators are fp32 either way.  batch <= 1024.
+ * bf16 lists met by many queries take the tensor-core kernel of elm_attend over a gathered bf16 copy (dense Q and O only).
+ * elm_cache4_attend_status: as elm_attend_status.
+ */
+int elm_cache4_attend_workspace_bytes(const elm_cache4_params *params, int32_t with_list, size_t *bytes);
+int elm_cache4_attend(const void *Q, const void *rows, const int32_t *table, const int32_t *length, const int32_t *cu,
+                      const int32_t *idx, const float *w, const elm_cache4_params *params, void *O, void *workspace,
+                      size_t workspace_bytes, void *stream);
+int elm_cache4_attend_status(const void *workspace, const elm_cache4_params *params, int32_t with_list, int32_t *status_host,
+                             void *stream);
+
+/*
  * End-to-end convenience call on HOST buffers: copies Q, K, V to the device, runs elm_compress and
  * elm_attend, copies O (and, when non-NULL, idx and w) back, and returns when everything has
  * arrived.  The host link bounds this call, so uploads, kernels and downloads overlap: K and V go

@@ -23,6 +23,8 @@ EXPORTED_SYMBOLS = [
     "elm_attend_workspace_bytes", "elm_attend_static", "elm_attend_static_status", "elm_compress_ragged_count", "elm_compress_ragged", "elm_express_workspace_bytes", "elm_express_compress",
     "elm_express_prefill_workspace_bytes", "elm_express_prefill",
     "elm_stream_workspace_bytes", "elm_stream_init", "elm_stream_step", "elm_stream_steps", "elm_stream_cache",
+    "elm_rope", "elm_rope_frequencies", "elm_page_plan", "elm_page_release", "elm_cache4_row_bytes", "elm_cache4_append", "elm_cache4_read",
+    "elm_cache4_attend_workspace_bytes", "elm_cache4_attend", "elm_cache4_attend_status",
     "elm_host_call_scratch_bytes", "elm_compress_attend_host",
     "elm_compress_status", "elm_attend_status", "elm_debug_set", "elm_debug_round_check", "elm_debug_decode_grid", "elm_debug_stream_form", "elm_profile_enable", "elm_profile_read", "elm_launch_count", "elm_strerror", "elm_version",
 ]
@@ -48,6 +50,40 @@ class ElmStream(ctypes.Structure):
         ("m", ctypes.c_int32), ("b", ctypes.c_int32), ("q", ctypes.c_int32), ("mbar", ctypes.c_int32),
         ("n_S", ctypes.c_int64 * 16), ("calls", ctypes.c_int64 * 16),
         ("n_known", ctypes.c_int64), ("seed", ctypes.c_uint64),
+    ]
+
+
+class RopeParams(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("inverse", ctypes.c_int32),
+        ("scale", ctypes.c_double), ("inv_freq", ctypes.POINTER(ctypes.c_double)),
+        ("x_stride", ctypes.c_int64 * 3), ("out_stride", ctypes.c_int64 * 3),
+    ]
+
+
+class PageParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+                ("max_tokens", ctypes.c_int32), ("n_free", ctypes.c_int32)]
+
+
+class AppendParams(ctypes.Structure):
+    _fields_ = [
+        ("n_tokens", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+        ("scale", ctypes.c_double), ("inv_freq", ctypes.POINTER(ctypes.c_double)),
+        ("q_stride", ctypes.c_int64 * 2), ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2),
+        ("q_out_stride", ctypes.c_int64 * 2),
+    ]
+
+
+class Cache4Params(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("n_kv", ctypes.c_int32), ("n_q", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("causal", ctypes.c_int32),
+        ("q_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3),
     ]
 
 
@@ -89,6 +125,18 @@ def load_library():
     lib.elm_stream_step.argtypes = [sp, vp, vp, vp, pp, vp, vp, sz, vp]
     lib.elm_stream_steps.argtypes = [sp, ctypes.c_int32, vp, vp, vp, pp, vp, vp, sz, vp]
     lib.elm_stream_cache.argtypes = [sp, pp, vp, vp, ctypes.POINTER(ctypes.c_int32), vp, sz, vp]
+    i32, i32p, f64, f64p = ctypes.c_int32, ctypes.POINTER(ctypes.c_int32), ctypes.c_double, ctypes.POINTER(ctypes.c_double)
+    gp, cp = ctypes.POINTER(PageParams), ctypes.POINTER(Cache4Params)
+    lib.elm_rope.argtypes = [vp, vp, ctypes.c_int64, ctypes.POINTER(RopeParams), vp, vp]
+    lib.elm_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, f64p, f64p]
+    lib.elm_page_plan.argtypes = [vp, vp, vp, vp, vp, gp, vp, vp, vp, vp, vp, vp, vp]
+    lib.elm_page_release.argtypes = [vp, vp, vp, vp, vp, gp, vp]
+    lib.elm_cache4_row_bytes.argtypes = [i32, szp]
+    lib.elm_cache4_append.argtypes = [vp, vp, vp, vp, vp, ctypes.POINTER(AppendParams), vp, vp, vp]
+    lib.elm_cache4_read.argtypes = [vp, vp, vp, vp, cp, vp, vp, vp]
+    lib.elm_cache4_attend_workspace_bytes.argtypes = [cp, i32, szp]
+    lib.elm_cache4_attend.argtypes = [vp, vp, vp, vp, vp, vp, vp, cp, vp, vp, sz, vp]
+    lib.elm_cache4_attend_status.argtypes = [vp, cp, i32, i32p, vp]
     lib.elm_host_call_scratch_bytes.argtypes = [pp, szp]
     lib.elm_compress_attend_host.argtypes = [vp, vp, vp, vp, vp, vp, pp, ctypes.c_uint64, vp, sz, vp]
     lib.elm_compress_status.argtypes = [vp, pp, ctypes.POINTER(ctypes.c_int32), vp]
@@ -382,6 +430,325 @@ def attend_static_status(Q, K, n_core: int, precision="fp32") -> int:
     out = ctypes.c_int32(-1)
     _check(load_library().elm_attend_static_status(ctypes.byref(p), n_core, ctypes.byref(out), _stream()),
            "elm_attend_static_status")
+    return int(out.value)
+
+
+# ------------------------------------------------------------------------------------------------
+# rotary positions, pages, rows held in 4 bits
+# ------------------------------------------------------------------------------------------------
+class _OnDevice:
+    """The calls below run on their tensors' device, on its current stream, whatever the current device is."""
+
+    def __init__(self, *tensors):
+        first = tensors[0]
+        for t in tensors:
+            if t is None:
+                continue
+            if not t.is_cuda:
+                if not torch.cuda.is_available():
+                    raise ElmError("no CUDA device: the library has no CPU fallback")
+                raise ElmError("tensors must be CUDA tensors")
+            if t.device != first.device:
+                raise ElmError("tensors must be on one device")
+        self.index = first.device.index
+        self.other = None
+
+    def __enter__(self):
+        if torch.cuda.current_device() != self.index:
+            self.other = torch.cuda.device(self.index)
+            self.other.__enter__()
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
+
+
+def _rows(x, dims, what):
+    """x with its last numbers side by side, and its other strides; a broadcast of one row is copied (strides of 0 mean dense)."""
+    if x.dim() != dims:
+        raise ElmError(f"{what} must have {dims} dimensions")
+    if x.numel() == 0:
+        raise ElmError(f"{what} is empty")
+    st = x.stride()
+    if st[-1] != 1 and x.shape[-1] > 1:
+        raise ElmError(f"{what}: the numbers of a head must lie side by side")
+    if not any(st[:-1]) and x.numel() > x.shape[-1]:
+        x = x.contiguous()
+        st = x.stride()
+    return x, st
+
+
+def _int32(t, what, shape=None):
+    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ElmError(f"{what} must be a contiguous int32 tensor" + (f" of shape {tuple(shape)}" if shape is not None else ""))
+    return t
+
+
+def _storage_code(t):
+    code = _dtype_code(t)
+    if code == ELM_E4M3:
+        raise ElmError(f"unsupported dtype {t.dtype}")
+    return code
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+_ROPE_LAYOUTS = {"halves": 0, "pairs": 1}
+_ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "smooth": 4}
+
+
+class Rope:
+    """Frequencies of a rotation (elm_rope_frequencies): the first ``rotary_dim`` numbers of a head turn in pairs, (i, i +
+    rotary_dim / 2) with layout "halves", (2i, 2i + 1) with "pairs".  ``scaling``: "plain", "linear", "base", "ramp" or "smooth",
+    with its ``factor``, the trained length ``original`` and the turns ``low`` and ``high`` of the blends (see include/elm.h)."""
+
+    def __init__(self, rotary_dim, base=10000.0, layout="halves", scaling="plain", factor=1.0, original=0.0, low=1.0, high=32.0):
+        if layout not in _ROPE_LAYOUTS or scaling not in _ROPE_SCALINGS:
+            raise ElmError(f"unknown layout {layout!r} or scaling {scaling!r}")
+        self.rotary_dim, self.layout = int(rotary_dim), _ROPE_LAYOUTS[layout]
+        self._freq = (ctypes.c_double * max(1, self.rotary_dim // 2))()
+        scale = ctypes.c_double(1.0)
+        _check(load_library().elm_rope_frequencies(self.rotary_dim, base, _ROPE_SCALINGS[scaling], factor, original, low, high, self._freq,
+                                                   ctypes.byref(scale)), "elm_rope_frequencies")
+        self.scale = scale.value
+        self._freq_ptr = ctypes.cast(self._freq, ctypes.POINTER(ctypes.c_double))
+
+    @property
+    def inv_freq(self):
+        return list(self._freq)
+
+
+def rope(X, positions, rope: Rope, inverse=False, out=None):
+    """elm_rope: X [B, H, n, d] (any strides, a head's numbers side by side) rotated by positions, an int32 tensor [B, n] or the first
+    position of every sequence; ``inverse``: rotated back (the gradient).  ``out``: X itself, or another tensor of its shape."""
+    lib = load_library()
+    tensors = [X, out, positions if isinstance(positions, torch.Tensor) else None]
+    with _OnDevice(*tensors):
+        X, xs = _rows(X, 4, "X")
+        B, H, n, d = X.shape
+        O = out if out is not None else torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        if O.shape != X.shape or O.dtype != X.dtype:
+            raise ElmError("out must have X's shape and dtype")
+        os_ = O.stride()
+        if out is not None:
+            if (os_[-1] != 1 and d > 1) or not any(os_[:-1]) and O.numel() > d:
+                raise ElmError("out: the numbers of a head must lie side by side, rows apart")
+        p = RopeParams(B, H, n, d, _storage_code(X), rope.rotary_dim, rope.layout, int(bool(inverse)), rope.scale, rope._freq_ptr)
+        p.x_stride[:] = xs[:3]
+        p.out_stride[:] = os_[:3]
+        if isinstance(positions, torch.Tensor):
+            pos, first = _int32(positions, "positions", (B, n)).data_ptr(), 0
+        else:
+            pos, first = None, int(positions)
+        _check(lib.elm_rope(X.data_ptr(), pos, first, ctypes.byref(p), O.data_ptr(), _stream()), "elm_rope")
+    return O
+
+
+class PagePlan:
+    """What page_plan() returns: start, length [B], free_count [1], cu [B + 1], positions, slots [max_tokens]."""
+
+    __slots__ = ("start", "length", "free_count", "cu", "positions", "slots")
+
+
+def page_plan(table, length, n_new, free, free_count, page_rows: int, max_tokens: int, length_out=None, free_count_out=None) -> PagePlan:
+    """elm_page_plan: pages, positions and slots of the n_new [B] tokens that come to requests of length [B].  ``table`` [B, max_pages]
+    gets the new pages' numbers; length_out and free_count_out may be length and free_count."""
+    lib = load_library()
+    with _OnDevice(table, length, n_new, free, free_count, length_out, free_count_out):
+        B, max_pages = _int32(table, "table").shape
+        _int32(length, "length", (B,)), _int32(n_new, "n_new", (B,)), _int32(free, "free"), _int32(free_count, "free_count", (1,))
+        # (one allocation for all that comes out; every part on a 16-byte boundary)
+        up = lambda n: -(-n // 4) * 4  # noqa: E731
+        need = 2 * up(B) + 4 + up(B + 1) + 2 * up(max_tokens)
+        buf = torch.empty(need, dtype=torch.int32, device=table.device)
+        at = 0
+
+        def part(n):
+            nonlocal at
+            t = buf[at:at + n]
+            at += up(n)
+            return t
+        r = PagePlan()
+        r.start, r.length, r.free_count, r.cu, r.positions, r.slots = part(B), part(B), part(1), part(B + 1), part(max_tokens), part(max_tokens)
+        if length_out is not None:
+            r.length = _int32(length_out, "length_out", (B,))
+        if free_count_out is not None:
+            r.free_count = _int32(free_count_out, "free_count_out", (1,))
+        p = PageParams(B, max_pages, page_rows, max_tokens, free.numel())
+        _check(lib.elm_page_plan(table.data_ptr(), length.data_ptr(), n_new.data_ptr(), free.data_ptr(), free_count.data_ptr(),
+                                 ctypes.byref(p), r.start.data_ptr(), r.length.data_ptr(), r.free_count.data_ptr(), r.cu.data_ptr(),
+                                 r.positions.data_ptr(), r.slots.data_ptr(), _stream()), "elm_page_plan")
+    return r
+
+
+def page_release(table, length, done, free, free_count, page_rows: int):
+    """elm_page_release: the pages of the requests with done [B] != 0 go back to the end of free; everything in place."""
+    lib = load_library()
+    with _OnDevice(table, length, done, free, free_count):
+        B, max_pages = _int32(table, "table").shape
+        _int32(length, "length", (B,)), _int32(done, "done", (B,)), _int32(free, "free"), _int32(free_count, "free_count", (1,))
+        p = PageParams(B, max_pages, page_rows, 0, free.numel())
+        _check(lib.elm_page_release(table.data_ptr(), length.data_ptr(), done.data_ptr(), free.data_ptr(), free_count.data_ptr(),
+                                    ctypes.byref(p), _stream()), "elm_page_release")
+
+
+def cache4_row_bytes(d: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load_library().elm_cache4_row_bytes(d, ctypes.byref(b)), "elm_cache4_row_bytes")
+    return int(b.value)
+
+
+def cache4_pool(n_pages: int, kv_heads: int, page_rows: int, d: int, device="cuda"):
+    """An empty pool of rows held in 4 bits: uint8 [n_pages, kv_heads, page_rows, row bytes]."""
+    return torch.empty(n_pages, kv_heads, page_rows, cache4_row_bytes(d), dtype=torch.uint8, device=device)
+
+
+def _pool_d(rows):
+    if rows.dtype != torch.uint8 or rows.dim() != 4 or not rows.is_contiguous():
+        raise ElmError("rows must be a contiguous uint8 tensor [n_pages, kv_heads, page_rows, row bytes]")
+    d = {80: 64, 144: 128}.get(rows.shape[3])
+    if d is None:
+        raise ElmError(f"rows of {rows.shape[3]} bytes are of no head dimension")
+    return d
+
+
+def cache4_append(rows, K, V, slots, rope: Rope = None, positions=None, Q=None, q_out=None):
+    """elm_cache4_append: K, V [T, Hkv, d] into the pool's rows slots [T] (a slot outside the pool: passed over), keys rotated by
+    ``rope`` at positions [T].  Q [T, Hq, d] comes back rotated (in q_out, which may be Q; of tokens passed over, as q_out was)."""
+    lib = load_library()
+    with _OnDevice(rows, K, V, slots, positions, Q, q_out):
+        d = _pool_d(rows)
+        K, ks = _rows(K, 3, "K")
+        V, vs = _rows(V, 3, "V")
+        T, H = K.shape[:2]
+        if K.shape != V.shape or K.dtype != V.dtype or K.shape[2] != d or H != rows.shape[1]:
+            raise ElmError("K and V must be [tokens, kv_heads, d] of the pool's heads, of one dtype")
+        _int32(slots, "slots", (T,))
+        if rope is not None:
+            if positions is None:
+                raise ElmError("a rotation needs positions")
+            _int32(positions, "positions", (T,))
+        p = AppendParams(T, 0, H, d, _storage_code(K), rows.shape[2], rows.shape[0])
+        if rope is not None:
+            p.rotary_dim, p.layout, p.scale, p.inv_freq = rope.rotary_dim, rope.layout, rope.scale, rope._freq_ptr
+        p.k_stride[:] = ks[:2]
+        p.v_stride[:] = vs[:2]
+        O = None
+        if Q is not None:
+            given = Q
+            Q, qs = _rows(Q, 3, "Q")
+            if Q.shape[0] != T or Q.shape[2] != d or Q.dtype != K.dtype:
+                raise ElmError("Q must be [tokens, q_heads, d] of K's dtype")
+            O = q_out if q_out is not None else torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+            if O.shape != Q.shape or O.dtype != Q.dtype or O.stride(2) != 1 or (O is given and Q is not given):
+                raise ElmError("q_out must have Q's shape and dtype, the numbers of a head side by side")
+            if not any(O.stride()[:2]) and O.numel() > d:
+                raise ElmError("q_out: rows must lie apart")
+            p.q_heads = Q.shape[1]
+            p.q_stride[:] = qs[:2]
+            p.q_out_stride[:] = O.stride()[:2]
+        _check(lib.elm_cache4_append(_ptr(Q), K.data_ptr(), V.data_ptr(), _ptr(positions) if rope is not None else None, slots.data_ptr(),
+                                     ctypes.byref(p), _ptr(O), rows.data_ptr(), _stream()), "elm_cache4_append")
+    return O
+
+
+def _cache4_params(rows, table, q_heads, dtype_code, n_kv, n_q=1, n_tokens=0, causal=True):
+    d = _pool_d(rows)
+    B, max_pages = _int32(table, "table").shape
+    return Cache4Params(B, q_heads, rows.shape[1], d, dtype_code, rows.shape[2], rows.shape[0], max_pages, n_kv, n_q, n_tokens, int(bool(causal)))
+
+
+def cache4_read(rows, table, n: int, idx=None, length=None, dtype=torch.bfloat16, out=None):
+    """elm_cache4_read -> K, V [B, Hkv, n, d]: rows 0 .. n - 1 of every request, or rows idx [B, Hkv, n]; a row that is not there (past
+    length [B], on no page) is zeros.  ``out``: a pair of tensors for them."""
+    lib = load_library()
+    with _OnDevice(rows, table, idx, length, *(out or ())):
+        code = {torch.float32: ELM_F32, torch.bfloat16: ELM_BF16}.get(dtype)
+        if code is None:
+            raise ElmError(f"unsupported dtype {dtype}")
+        p = _cache4_params(rows, table, rows.shape[1], code, n)
+        shape = (p.batch, p.kv_heads, n, p.d)
+        if idx is not None:
+            _int32(idx, "idx", shape[:3])
+        if length is not None:
+            _int32(length, "length", shape[:1])
+        K, V = out if out is not None else (torch.empty(shape, dtype=dtype, device=rows.device), torch.empty(shape, dtype=dtype, device=rows.device))
+        if out is not None and any(tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() for t in out):
+            raise ElmError(f"out must be two contiguous tensors of shape {shape} and dtype {dtype}")
+        _check(lib.elm_cache4_read(rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(idx), ctypes.byref(p), K.data_ptr(), V.data_ptr(),
+                                   _stream()), "elm_cache4_read")
+    return K, V
+
+
+def _attend4_params(Q, rows, table, cu, idx, w, length, n_kv, max_q, causal, out):
+    if (idx is None) == (length is None):
+        raise ElmError("give either length (a request's rows) or idx and w (a list of them)")
+    Q, qs = _rows(Q, 3 if cu is not None else 4, "Q")
+    if cu is not None:
+        if max_q is None:
+            raise ElmError("cu needs max_q, the most tokens of any request")
+        T, Hq, d = Q.shape
+        p = _cache4_params(rows, table, Hq, _storage_code(Q), 0, max_q, T, causal)
+        _int32(cu, "cu", (p.batch + 1,))
+        qs = (0, qs[1], qs[0])
+    else:
+        B, Hq, n_q, d = Q.shape
+        p = _cache4_params(rows, table, Hq, _storage_code(Q), 0, n_q, 0, causal)
+        if B != p.batch:
+            raise ElmError("Q and table must have one batch")
+        qs = qs[:3]
+    if d != p.d:
+        raise ElmError("Q must have the pool's head dimension")
+    if idx is not None:
+        if cu is not None or w is None or w.dtype != torch.float32 or not w.is_contiguous() or idx.shape != w.shape:
+            raise ElmError("idx goes with w, a contiguous float32 tensor of its shape, and with Q [B, Hq, n, d]")
+        p.n_kv = _int32(idx, "idx").shape[-1]
+        if tuple(idx.shape) != (p.batch, p.kv_heads, p.n_kv):
+            raise ElmError("idx must be [B, Hkv, n]")
+    else:
+        _int32(length, "length", (p.batch,))
+        p.n_kv = int(n_kv) if n_kv is not None else 0
+    O = out if out is not None else torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if O.shape != Q.shape or O.dtype != Q.dtype or (O.stride(-1) != 1) or (not any(O.stride()[:-1]) and O.numel() > d):
+        raise ElmError("out must have Q's shape and dtype, the numbers of a head side by side")
+    os_ = O.stride()
+    # dense tensors are told to the library as such: its tensor-core form takes no others
+    if cu is not None or not Q.is_contiguous():
+        p.q_stride[:] = qs
+    if cu is not None:
+        p.o_stride[:] = (0, os_[1], os_[0])
+    elif not O.is_contiguous():
+        p.o_stride[:] = os_[:3]
+    return Q, O, p
+
+
+def cache4_attend_workspace_bytes(params: Cache4Params, with_list: bool) -> int:
+    need = ctypes.c_size_t(0)
+    _check(load_library().elm_cache4_attend_workspace_bytes(ctypes.byref(params), int(with_list), ctypes.byref(need)),
+           "elm_cache4_attend_workspace_bytes")
+    return int(need.value)
+
+
+def cache4_attend(Q, rows, table, length=None, idx=None, w=None, cu=None, max_q=None, n_kv=None, causal=True, workspace=None, out=None):
+    """elm_cache4_attend: Q [B, Hq, n, d] over the rows of the requests of table [B, max_pages]: the first length [B] of them (n_kv: a bound
+    of the lengths that the host knows; causal: a request's queries are its last tokens), or the list idx with weights w
+    [B, Hkv, n_core].  With cu [B + 1]: Q [T, Hq, d], request b has the tokens cu[b] .. cu[b + 1] - 1, max_q at most.  O like Q."""
+    lib = load_library()
+    with _OnDevice(rows, Q, table, length, idx, w, cu, workspace, out):
+        Q, O, p = _attend4_params(Q, rows, table, cu, idx, w, length, n_kv, max_q, causal, out)
+        ws = workspace if workspace is not None else _workspace(cache4_attend_workspace_bytes(p, idx is not None), Q.device)
+        _check(lib.elm_cache4_attend(Q.data_ptr(), rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(cu), _ptr(idx), _ptr(w),
+                                     ctypes.byref(p), O.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "elm_cache4_attend")
+    return O
+
+
+def cache4_attend_status(workspace, params: Cache4Params, with_list: bool) -> int:
+    """elm_cache4_attend_status: 0 unless a bounded device wait expired during the last cache4_attend call with this workspace."""
+    out = ctypes.c_int32(-1)
+    _check(load_library().elm_cache4_attend_status(workspace.data_ptr(), ctypes.byref(params), int(with_list), ctypes.byref(out), _stream()),
+           "elm_cache4_attend_status")
     return int(out.value)
 
 

@@ -37,7 +37,12 @@ AttendLayout attend_layout(const elm_params *p, int32_t n_core);
 // Block lists (with lifetimes, tensor-core path only): when `tile_cnt` is set, pair x of 128-query tiles (rows
 // 256 x ... of every head) streams only the tile_cnt[x] blocks tile_blk[x * tile_cap + 0 ...] of the list; the
 // caller guarantees that every entry some row of the pair sees lies in one of them.
+//
+// Rows in 4 bits (tensor-core path): when `pool4` is set, the list's rows are those of that pool and K and V are not used; an
+// entry whose row is not there, or whose weight is not above 0, is not seen.
+struct Pool4;
 struct AttendWindow {
+    const Pool4 *pool4 = nullptr;
     int64_t q_row0 = 0;
     int64_t n_q_total = 0;               // 0: params->n_q
     int32_t tail_start = 0x7fffffff;     // no tail

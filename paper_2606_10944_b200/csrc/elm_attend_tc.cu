@@ -42,6 +42,7 @@
 #include <type_traits>
 
 #include "elm_attend.cuh"
+#include "elm_cache4.cuh"
 #include "elm_common.cuh"
 #include "elm_sm100.cuh"
 
@@ -183,6 +184,80 @@ __global__ void __launch_bounds__(256) gather_tc_kernel(const __nv_bfloat16 *__r
     if (differs) atomicOr(nonuniform + p, 1);
     __syncthreads();
     // transposed write: a warp writes the 64 entries of one dimension e, 128 contiguous bytes
+    for (int e = warp; e < D; e += 8) {
+        const uint32_t lo = __bfloat16_as_ushort(tile[2 * lane][e]), hi = __bfloat16_as_ushort(tile[2 * lane + 1][e]);
+        *reinterpret_cast<uint32_t *>(Vt + (((int64_t)p * (n_pad / 128) + c0 / 128) * D + e) * 128 + (c0 % 128) + 2 * lane) = lo | (hi << 16);
+    }
+}
+
+// The same of rows held in 4 bits: their numbers as bf16, exactly.  An entry that is not there is a padded column.
+template <int D>
+__global__ void __launch_bounds__(256) gather4_tc_kernel(Pool4 pool, const int32_t *__restrict__ idx, const float *__restrict__ w, int n_core,
+                                                         int n_pad, __nv_bfloat16 *__restrict__ Kc, __nv_bfloat16 *__restrict__ Vt,
+                                                         __nv_bfloat16 *__restrict__ Bx, float inv_scale_log2, int *__restrict__ nonuniform)
+{
+    using R = Row4<D>;
+    __shared__ __align__(16) __nv_bfloat16 tile[GATHER_COLS][D + 8];
+    const int p = blockIdx.y, b = p / pool.kv_heads, h = p % pool.kv_heads;
+    const int c0 = blockIdx.x * GATHER_COLS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float w0 = w[(int64_t)p * n_core];
+    bool differs = false;
+    uint32_t row_mine = NO_ROW;
+    float w_mine = 0.f;
+    if (lane < GATHER_COLS / 8 && c0 + warp + 8 * lane < n_core) {
+        const int64_t at = (int64_t)p * n_core + c0 + warp + 8 * lane;
+        w_mine = w[at];
+        if (w_mine > 0.f) row_mine = pool_row(pool, b, h, idx[at]);
+    }
+    // a problem none of whose entries is there: its columns must not be hidden all (the attention takes the distance to the largest logit,
+    // and -1e30 is so large that its own rounding would be one); with logits and values of 0 its outputs are 0
+    float hidden = -1e30f;
+    if (!__syncthreads_or(row_mine != NO_ROW)) {
+        int any = 0;
+        for (int e0 = 0; e0 < n_core && !any; e0 += 256) {
+            const int64_t at = (int64_t)p * n_core + e0 + threadIdx.x;
+            any = __syncthreads_or(e0 + (int)threadIdx.x < n_core && w[at] > 0.f && pool_row(pool, b, h, idx[at]) != NO_ROW);
+        }
+        if (!any) hidden = 0.f;
+    }
+    const int chunk = lane & 15;                               // eight numbers of the key (lanes 0 .. 15), of the value
+#pragma unroll 4
+    for (int i = 0; i < GATHER_COLS / 8; ++i) {
+        const int r = warp + 8 * i, c = c0 + r;
+        const uint32_t row = __shfl_sync(0xffffffffu, row_mine, i);
+        const float wc = __shfl_sync(0xffffffffu, w_mine, i);
+        const bool ok = row != NO_ROW;
+        if (chunk < D / 8) {
+            uint32_t x[4] = {0u, 0u, 0u, 0u};
+            if (ok) {
+                const unsigned char *from = pool.rows + (uint64_t)row * R::BYTES;
+                const int j = (lane >> 4) * (D / 8) + chunk;
+                codes8_to_half2(*reinterpret_cast<const uint32_t *>(from + 4 * j), x);
+                const uint32_t s = scale4_half_bits(from[R::SCALES + j / 2]) * 0x10001u;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t y = hmul2_bits(x[k], s);
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&y));
+                    x[k] = pack_bf16x2(f.x, f.y);
+                }
+            }
+            const uint4 v = make_uint4(x[0], x[1], x[2], x[3]);
+            if (lane < 16) reinterpret_cast<uint4 *>(Kc + ((int64_t)p * n_pad + c) * D)[chunk] = v;
+            else *reinterpret_cast<uint4 *>(&tile[r][chunk * 8]) = v;
+        }
+        if (lane < 16) {
+            const float x = ok ? log2f(wc) * inv_scale_log2 : hidden;
+            const __nv_bfloat16 hi = __float2bfloat16(x);
+            const float r1 = ok ? x - __bfloat162float(hi) : 0.f;
+            const __nv_bfloat16 mid = __float2bfloat16(r1);
+            const __nv_bfloat16 lo = __float2bfloat16(r1 - __bfloat162float(mid));
+            Bx[((int64_t)p * n_pad + c) * 16 + lane] = lane == 0 ? hi : (lane == 1 ? mid : (lane == 2 ? lo : __float2bfloat16(0.f)));
+            if (lane == 0 && c < n_core && (!ok || wc != w0)) differs = true;
+        }
+    }
+    if (differs) atomicOr(nonuniform + p, 1);
+    __syncthreads();
     for (int e = warp; e < D; e += 8) {
         const uint32_t lo = __bfloat16_as_ushort(tile[2 * lane][e]), hi = __bfloat16_as_ushort(tile[2 * lane + 1][e]);
         *reinterpret_cast<uint32_t *>(Vt + (((int64_t)p * (n_pad / 128) + c0 / 128) * D + e) * 128 + (c0 % 128) + 2 * lane) = lo | (hi << 16);
@@ -1160,8 +1235,12 @@ static int launch(const __nv_bfloat16 *Q, const __nv_bfloat16 *K, const __nv_bfl
     {
         StageTimer t(timed ? ELM_STAGE_GATHER : -1, st, 1);
         ELM_CUDA_TRY(cudaMemsetAsync(flags, 0, sizeof(int) * (size_t)(problems + 1), st));
-        gather_tc_kernel<D><<<dim3((unsigned)(n_pad / GATHER_COLS), (unsigned)problems), 256, 0, st>>>(
-            K, V, idx, w, p->n_kv, n_core, n_pad, Kc, Vt, Bx, 1.f / scale_log2, flags);
+        if (win.pool4)
+            gather4_tc_kernel<D><<<dim3((unsigned)(n_pad / GATHER_COLS), (unsigned)problems), 256, 0, st>>>(
+                *win.pool4, idx, w, n_core, n_pad, Kc, Vt, Bx, 1.f / scale_log2, flags);
+        else
+            gather_tc_kernel<D><<<dim3((unsigned)(n_pad / GATHER_COLS), (unsigned)problems), 256, 0, st>>>(
+                K, V, idx, w, p->n_kv, n_core, n_pad, Kc, Vt, Bx, 1.f / scale_log2, flags);
         count_launches(1);
         ELM_CUDA_TRY(cudaGetLastError());
     }

@@ -1,0 +1,354 @@
+// New tokens into a pool of rows held in 4 bits (elm_cache4_append), and rows back (elm_cache4_read).
+//
+// Both are one pass over their rows.  Append reads 2 d numbers per token and KV head and writes a row (144 bytes at d = 128), besides the queries'
+// 2 d per query head; read the other way round.  HBM-bound in long calls, bound by the launch in a decode step.
+#include "elm_cache4.cuh"
+#include "elm_rope.cuh"
+
+namespace elm {
+namespace {
+
+constexpr int APP_THREADS = 256;
+constexpr int APP_TILE = 32;             // tokens of a CTA at most
+
+struct AppendArgs {
+    const void *q, *k, *v;
+    void *q_out;
+    const int32_t *positions, *slots;
+    unsigned char *rows;
+    int64_t qs[2], ks[2], vs[2], qos[2];
+    double scale;
+    int32_t n_tokens, q_heads, kv_heads, rotary, page_shift, tile;
+    uint32_t n_slots;
+};
+
+// the 16 numbers from `first` on of a head's row, rotated where they are rotated
+template <typename T, bool WIDE>
+__device__ __forceinline__ void load_group(const T *row, int first, float (&x)[C4_GROUP])
+{
+    if constexpr (WIDE) {
+        constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < C4_GROUP / E; ++i) {
+            Chunk<T, E> c;
+            c.load(row + first + i * E);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[i * E + e] = c.v[e];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < C4_GROUP; ++i) x[i] = load_as<float>(row, first + i);
+    }
+}
+
+// HALVES with a group that lies in one half whose partners start on a 16-byte boundary (WIDE): the partners are loaded alike; any other
+// group number by number.  A partner is loaded by the other half's thread as well: from L1.
+template <typename T, bool WIDE, bool HALVES>
+__device__ __forceinline__ void rotate_group(const T *row, int first, int rotary, const float2 *cs, float (&x)[C4_GROUP])
+{
+    if (first >= rotary) return;
+    const int half = rotary / 2;
+    if constexpr (!HALVES) {
+#pragma unroll
+        for (int i = 0; i < C4_GROUP; i += 2)
+            if (first + i < rotary) rope_turn(x[i], x[i + 1], cs[(first + i) / 2]);
+    } else if (WIDE && half % C4_GROUP == 0) {
+        float y[C4_GROUP];
+        const bool lower = first < half;
+        load_group<T, true>(row, lower ? first + half : first - half, y);
+        const float2 *c = cs + (lower ? first : first - half);
+#pragma unroll
+        for (int i = 0; i < C4_GROUP; ++i) {
+            float a = lower ? x[i] : y[i], b = lower ? y[i] : x[i];
+            rope_turn(a, b, c[i]);
+            x[i] = lower ? a : b;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < C4_GROUP; ++i) {
+            const int j = first + i;
+            if (j < half) {
+                float b = load_as<float>(row, j + half);
+                rope_turn(x[i], b, cs[j]);
+            } else if (j < rotary) {
+                float a = load_as<float>(row, j - half);
+                rope_turn(a, x[i], cs[j - half]);
+            }
+        }
+    }
+}
+
+// A thread takes a group of 16 numbers: of a query (rotated, stored as it is), a key or a value (made a code).  The groups of a row are
+// neighbouring lanes, so that a row's codes leave in one piece; four lanes put their scales together.
+template <typename T, int D, bool WIDE, bool HALVES>
+__global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTurns turns)
+{
+    using R = Row4<D>;
+    constexpr int G = R::GROUPS;
+    extern __shared__ float2 cs[];                             // [tile][rotary / 2]
+    cudaGridDependencySynchronize();
+    const int pairs = a.rotary / 2;
+    const int t0 = blockIdx.x * a.tile;
+    const int count = min(a.tile, a.n_tokens - t0);
+    for (int i = threadIdx.x; i < count * pairs; i += APP_THREADS) {
+        const int t = i / pairs;
+        cs[i] = rope_cos_sin(a.positions[t0 + t], turns.turn[i - t * pairs], a.scale, a.scale);
+    }
+    __syncthreads();
+    const int per_token = (2 * a.kv_heads + a.q_heads) * G;
+    const int total = count * per_token;
+    // (whole warps stay together: the lanes of a row exchange their scales)
+    for (int i0 = threadIdx.x & ~31; i0 < total; i0 += APP_THREADS) {
+        const int i = i0 + (threadIdx.x & 31);
+        const bool live = i < total;
+        const int t = live ? i / per_token : 0, r = live ? i - t * per_token : 0;
+        const uint32_t slot = (uint32_t)a.slots[t0 + t];
+        const bool there = live && slot < a.n_slots;
+        const float2 *c = cs + t * pairs;
+        const int64_t tok = t0 + t;
+        const int kv_items = 2 * a.kv_heads * G;
+        uint32_t byte = 0;
+        unsigned char *row = nullptr;
+        int j = 0;
+        if (there && r < kv_items) {
+            const int h = r / (2 * G);
+            j = r - h * 2 * G;                                 // the row's group: keys, then values
+            const bool key = j < G;
+            const T *src = key ? (const T *)a.k + tok * a.ks[0] + h * a.ks[1] : (const T *)a.v + tok * a.vs[0] + h * a.vs[1];
+            const int first = (key ? j : j - G) * C4_GROUP;
+            float x[C4_GROUP];
+            load_group<T, WIDE>(src, first, x);
+            if (key) rotate_group<T, WIDE, HALVES>(src, first, a.rotary, c, x);
+            uint2 codes;
+            byte = quantise4(x, codes);
+            const uint32_t page = slot >> a.page_shift, in_page = slot & ((1u << a.page_shift) - 1u);
+            row = a.rows + ((((uint64_t)page * (uint32_t)a.kv_heads + h) << a.page_shift) + in_page) * R::BYTES;
+            *reinterpret_cast<uint2 *>(row + j * 8) = codes;
+        } else if (there) {
+            const int q = r - kv_items, h = q / G, first = (q - h * G) * C4_GROUP;
+            const T *src = (const T *)a.q + tok * a.qs[0] + h * a.qs[1];
+            T *dst = (T *)a.q_out + tok * a.qos[0] + h * a.qos[1];
+            if (HALVES && WIDE && a.rotary / 2 % C4_GROUP == 0) {
+                // a thread of the lower half takes both groups of its pairs, so that queries may be rotated in place
+                const int half = a.rotary / 2;
+                if (first < half || first >= a.rotary) {
+                    float x[C4_GROUP], y[C4_GROUP];
+                    const bool turn = first < half;
+                    load_group<T, true>(src, first, x);
+                    if (turn) {
+                        load_group<T, true>(src, first + half, y);
+#pragma unroll
+                        for (int e = 0; e < C4_GROUP; ++e) rope_turn(x[e], y[e], c[first + e]);
+                    }
+                    constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+                    for (int e = 0; e < C4_GROUP; e += E) {
+                        Chunk<T, E> u, w;
+#pragma unroll
+                        for (int k = 0; k < E; ++k) {
+                            u.v[k] = x[e + k];
+                            if (turn) w.v[k] = y[e + k];
+                        }
+                        u.store(dst + first + e);
+                        if (turn) w.store(dst + first + half + e);
+                    }
+                }
+            } else if (HALVES) {
+                // pair by pair: this thread the pairs whose first number is in its group, and what is not rotated
+                const int half = a.rotary / 2;
+                for (int e = first; e < first + C4_GROUP; ++e) {
+                    if (e < half) {
+                        float x = load_as<float>(src, e), y = load_as<float>(src, e + half);
+                        rope_turn(x, y, c[e]);
+                        store_from(dst, e, x);
+                        store_from(dst, e + half, y);
+                    } else if (e >= a.rotary) {
+                        store_from(dst, e, load_as<float>(src, e));
+                    }
+                }
+            } else {
+                float x[C4_GROUP];
+                load_group<T, WIDE>(src, first, x);
+                rotate_group<T, WIDE, false>(src, first, a.rotary, c, x);
+                constexpr int E = WIDE ? 16 / (int)sizeof(T) : 1;
+#pragma unroll
+                for (int e = 0; e < C4_GROUP; e += E) {
+                    Chunk<T, E> u;
+#pragma unroll
+                    for (int k = 0; k < E; ++k) u.v[k] = x[e + k];
+                    u.store(dst + first + e);
+                }
+            }
+        }
+        // scales: a row's lanes are neighbours and start at a multiple of 4 lanes, so four of them fill a word
+        uint32_t word = byte << (8 * (j & 3));
+        word |= __shfl_xor_sync(0xffffffffu, word, 1);
+        word |= __shfl_xor_sync(0xffffffffu, word, 2);
+        if (row && (j & 3) == 0) {
+            *reinterpret_cast<uint32_t *>(row + R::SCALES + j) = word;
+            if (2 * G + R::SCALES < R::BYTES && j == 0) *reinterpret_cast<uint2 *>(row + R::SCALES + 2 * G) = make_uint2(0u, 0u);
+        }
+    }
+}
+
+struct ReadArgs {
+    Pool4 pool;
+    const int32_t *length, *idx;
+    void *k, *v;
+    int32_t n;
+    int64_t rows;                        // batch * kv_heads * n
+};
+
+// A thread makes 8 numbers (4 bytes of codes): 16 bytes of bf16, so that a warp's stores are whole lines.
+template <typename T, int D> __global__ void __launch_bounds__(256) read4_kernel(const __grid_constant__ ReadArgs a)
+{
+    using R = Row4<D>;
+    constexpr int PER_ROW = 2 * D / 8;
+    cudaGridDependencySynchronize();
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t out_row = i / PER_ROW;
+    if (out_row >= a.rows) return;
+    const int j = (int)(i % PER_ROW);
+    const int64_t problem = out_row / a.n;
+    const int64_t e = out_row - problem * a.n;
+    const int b = (int)(problem / a.pool.kv_heads), h = (int)(problem - (int64_t)b * a.pool.kv_heads);
+    const int64_t r = a.idx ? a.idx[out_row] : e;
+    uint32_t row = r < 0 || (a.length && r >= a.length[b]) ? NO_ROW : pool_row(a.pool, b, h, r);
+    uint32_t half2s[4] = {0u, 0u, 0u, 0u};
+    if (row != NO_ROW) {
+        const unsigned char *p = a.pool.rows + (uint64_t)row * R::BYTES;
+        const uint32_t codes = *reinterpret_cast<const uint32_t *>(p + 4 * j);
+        const uint32_t s = scale4_half_bits(p[R::SCALES + j / 2]) * 0x10001u;
+        codes8_to_half2(codes, half2s);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) half2s[k] = hmul2_bits(half2s[k], s);
+    }
+    T *out = (T *)(j < PER_ROW / 2 ? a.k : a.v) + out_row * D + (j % (PER_ROW / 2)) * 8;
+    constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int k = 0; k < 8; k += E) {
+        Chunk<T, E> c;
+#pragma unroll
+        for (int x = 0; x < E; x += 2) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&half2s[(k + x) / 2]));
+            c.v[x] = f.x;
+            c.v[x + 1] = f.y;
+        }
+        c.store(out + k);
+    }
+}
+
+template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &turns, bool halves, bool wide, cudaStream_t st)
+{
+    const int per_token = (2 * a.kv_heads + a.q_heads) * (D / C4_GROUP);
+    // tokens per CTA: two rounds of its threads (a token's cosines are formed once for all its heads), fewer where the tokens would
+    // not fill the GPU
+    int tile = (2 * APP_THREADS + per_token - 1) / per_token;
+    const int fill = a.n_tokens / (4 * device_sm_count());
+    if (tile > fill) tile = fill < 1 ? 1 : fill;
+    if (tile > APP_TILE) tile = APP_TILE;
+    a.tile = tile;
+    const size_t smem = (size_t)tile * (a.rotary / 2) * sizeof(float2);
+    const dim3 grid((unsigned)(((int64_t)a.n_tokens + tile - 1) / tile));
+    auto kern = wide ? (halves ? append4_kernel<T, D, true, true> : append4_kernel<T, D, true, false>)
+                     : (halves ? append4_kernel<T, D, false, true> : append4_kernel<T, D, false, false>);
+    ELM_CUDA_TRY(launch_after(kern, grid, dim3(APP_THREADS), smem, st, a, turns));
+    count_launches(1);
+    return cuda_status(cudaGetLastError());
+}
+
+}  // namespace
+}  // namespace elm
+
+using namespace elm;
+
+extern "C" int elm_cache4_row_bytes(int32_t d, size_t *bytes)
+{
+    if (!bytes) return ELM_ERR_NULL;
+    if (d != 64 && d != 128) return ELM_ERR_SHAPE;
+    *bytes = (size_t)row4_bytes(d);
+    return ELM_OK;
+}
+
+extern "C" int elm_cache4_append(const void *Q, const void *K, const void *V, const int32_t *positions, const int32_t *slots,
+                                 const elm_append_params *p, void *Q_out, void *rows, void *stream)
+{
+    if (!p || !K || !V || !slots || !rows) return ELM_ERR_NULL;
+    if (p->dtype != ELM_F32 && p->dtype != ELM_BF16) return ELM_ERR_DTYPE;
+    if (p->n_tokens < 1 || p->q_heads < 0 || p->kv_heads < 1 || (p->d != 64 && p->d != 128)) return ELM_ERR_SHAPE;
+    if (p->q_heads > 65535 || p->kv_heads > 65535) return ELM_ERR_SHAPE;
+    const int shift = page_shift_of(p->page_rows);
+    if (shift < 0 || !pool_fits(p->n_pages, p->page_rows, p->kv_heads)) return ELM_ERR_SHAPE;
+    if (p->rotary_dim < 0 || p->rotary_dim > p->d || (p->rotary_dim & 1)) return ELM_ERR_SHAPE;
+    if (p->layout != ELM_ROPE_HALVES && p->layout != ELM_ROPE_PAIRS) return ELM_ERR_SHAPE;
+    if (p->q_heads > 0 && (!Q || !Q_out)) return ELM_ERR_NULL;
+    RopeTurns turns;
+    if (p->rotary_dim > 0) {
+        if (!positions || !p->inv_freq) return ELM_ERR_NULL;
+        if (!isfinite(p->scale) || !rope_turns(p->inv_freq, p->rotary_dim / 2, turns)) return ELM_ERR_SHAPE;
+    }
+    const int item = (int)elt_bytes(p->dtype);
+    AppendArgs a = {};
+    a.q = Q;
+    a.k = K;
+    a.v = V;
+    a.q_out = Q_out;
+    a.positions = positions;
+    a.slots = slots;
+    a.rows = (unsigned char *)rows;
+    auto strides = [&](const int64_t (&in)[2], int heads, int64_t (&out)[2]) {
+        const bool dense = in[0] == 0 && in[1] == 0;
+        out[0] = dense ? (int64_t)heads * p->d : in[0];
+        out[1] = dense ? p->d : in[1];
+        return out[0] | out[1];
+    };
+    int64_t all = strides(p->k_stride, p->kv_heads, a.ks) | strides(p->v_stride, p->kv_heads, a.vs);
+    uintptr_t at = (uintptr_t)K | (uintptr_t)V;
+    if (p->q_heads > 0) {
+        all |= strides(p->q_stride, p->q_heads, a.qs) | strides(p->q_out_stride, p->q_heads, a.qos);
+        at |= (uintptr_t)Q | (uintptr_t)Q_out;
+        // rows of Q_out that would be written twice; in place only where every number stays in its place
+        if ((p->n_tokens > 1 && a.qos[0] == 0) || (p->q_heads > 1 && a.qos[1] == 0)) return ELM_ERR_SHAPE;
+        if (Q == Q_out && (a.qs[0] != a.qos[0] || a.qs[1] != a.qos[1])) return ELM_ERR_SHAPE;
+    }
+    if ((at & (item - 1)) || (((uintptr_t)positions | (uintptr_t)slots) & 3) || ((uintptr_t)rows & 15)) return ELM_ERR_ALIGN;
+    a.scale = p->scale;
+    a.n_tokens = p->n_tokens;
+    a.q_heads = p->q_heads;
+    a.kv_heads = p->kv_heads;
+    a.rotary = p->rotary_dim;
+    a.page_shift = shift;
+    a.n_slots = (uint32_t)((int64_t)p->n_pages << shift);
+    const bool wide = !(at & 15) && all % (16 / item) == 0, halves = p->layout == ELM_ROPE_HALVES;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (p->dtype == ELM_BF16)
+        return p->d == 64 ? launch_append<__nv_bfloat16, 64>(a, turns, halves, wide, st) : launch_append<__nv_bfloat16, 128>(a, turns, halves, wide, st);
+    return p->d == 64 ? launch_append<float, 64>(a, turns, halves, wide, st) : launch_append<float, 128>(a, turns, halves, wide, st);
+}
+
+extern "C" int elm_cache4_read(const void *rows, const int32_t *table, const int32_t *length, const int32_t *idx, const elm_cache4_params *p,
+                               void *K_out, void *V_out, void *stream)
+{
+    if (!p || !rows || !table || !K_out || !V_out) return ELM_ERR_NULL;
+    if (p->dtype != ELM_F32 && p->dtype != ELM_BF16) return ELM_ERR_DTYPE;
+    if (p->batch < 1 || p->kv_heads < 1 || p->kv_heads > 65535 || p->n_kv < 1 || p->max_pages < 1 || (p->d != 64 && p->d != 128)) return ELM_ERR_SHAPE;
+    const int shift = page_shift_of(p->page_rows);
+    if (shift < 0 || !pool_fits(p->n_pages, p->page_rows, p->kv_heads)) return ELM_ERR_SHAPE;
+    if (((uintptr_t)rows | (uintptr_t)K_out | (uintptr_t)V_out) & 15) return ELM_ERR_ALIGN;
+    if (((uintptr_t)table | (uintptr_t)length | (uintptr_t)idx) & 3) return ELM_ERR_ALIGN;
+    ReadArgs a;
+    a.pool = Pool4{(const unsigned char *)rows, table, p->n_pages, p->max_pages, shift, p->kv_heads};
+    a.length = length;
+    a.idx = idx;
+    a.k = K_out;
+    a.v = V_out;
+    a.n = p->n_kv;
+    a.rows = (int64_t)p->batch * p->kv_heads * p->n_kv;
+    const int64_t ctas = (a.rows * (2 * p->d / 8) + 255) / 256;
+    if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
+    auto kern = p->dtype == ELM_BF16 ? (p->d == 64 ? read4_kernel<__nv_bfloat16, 64> : read4_kernel<__nv_bfloat16, 128>)
+                                     : (p->d == 64 ? read4_kernel<float, 64> : read4_kernel<float, 128>);
+    ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)ctas), dim3(256), 0, (cudaStream_t)stream, a));
+    count_launches(1);
+    return cuda_status(cudaGetLastError());
+}

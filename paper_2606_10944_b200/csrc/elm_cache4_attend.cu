@@ -1,0 +1,817 @@
+// Attention over rows held in 4 bits (elm_cache4_attend): a request's rows up to its length, or a weighted list of them.
+//
+//   O[j,:] = sum_c w_c exp(<q_j,k_c>/sqrt(d)) v_c / sum_c w_c exp(<q_j,k_c>/sqrt(d))      Eq. (def:att_approx)
+//
+// A problem is N = 8 or 16 query vectors of one KV head (its query heads, and neighbouring tokens) over that head's rows.  A warp takes
+// 32 rows at a time.  Both contractions run on mma.sync m16n8k16 with fp16 operands and fp32 accumulators and with the QUERY VECTORS as
+// the narrow side, so that the few there are fill it:
+//   S^T = K Q^T   (16 rows x 8 vectors):  a lane's part of the K operand is one stretch of 32 numbers (d = 64: 16) of rows g and g + 8, read as
+//                 16 (8) bytes of codes; which numbers make up a step of the contraction is free as long as Q is laid out alike.
+//   O^T = V^T P^T (16 numbers x 8 vectors): the V operand wants two neighbouring rows' numbers in one register: nibbles of the two
+//                 rows' words are put side by side (two logic operations per eight numbers), so that converting a byte gives the pair.
+//                 P^T comes from the accumulator layout of S^T by one 8x8 transposition (movmatrix) per 16 rows and half.
+// Codes become fp16 numbers by one conversion per two and are multiplied by their scales, exactly (elm_cache4.cuh).  A query vector is scaled to
+// a largest magnitude of 2^11 .. 2^12 before it is rounded to fp16 (bf16 numbers have fewer bits: exact but for those 2^-25 below the
+// largest); probabilities are exp2 of the distance to a running reference + 8, so that fp16 holds them down to 2^-32 of the largest, and the
+// reference moves only when the maximum has passed it by 2^6.  fp32 queries and outputs: queries and probabilities as two fp16 parts (22
+// bits), and each tile's sums go to fp32 accumulators by ordinary additions, since the matrix instruction cuts off low bits.
+//
+// What bounds it: reading each row once (144 bytes at d = 128).  The rows of all problems form one line of tiles, and every CTA takes an equal
+// stretch of it, whatever the requests' lengths are - they are on the device, and the stretch is found there.  A problem that lies in one
+// stretch is finished there; the parts of one that several CTAs share go to the workspace and are joined by a second launch.
+#include <math.h>
+
+#include "elm_attend.cuh"
+#include "elm_cache4.cuh"
+
+namespace elm {
+namespace {
+
+constexpr int A4_WARPS = 4;
+constexpr int A4_THREADS = 32 * A4_WARPS;
+constexpr int A4_TILE = 32;              // rows of a warp's tile
+constexpr int A4_STAGES = 3;
+constexpr int A4_MAX_BATCH = 1024;
+constexpr int A4_CTA_TILES = A4_WARPS;   // a CTA's stretch holds at least these
+constexpr float A4_LIFT = 8.f;           // probabilities are 2^8 times their share of the reference's
+constexpr float A4_SLACK = 6.f;          // how far the maximum may pass the reference: fp16 ends at 2^16
+
+struct Attend4Args {
+    Pool4 pool;
+    const void *q;
+    void *o;
+    const int32_t *length, *cu, *idx;
+    const float *w;
+    float *part;                         // [2 * ctas][N][D + 2]
+    int64_t qs[3], os[3];
+    int32_t batch, q_heads, rep, n_kv, n_q, n_tokens, causal;
+};
+
+// Where the problems of every request begin in the line of tiles.  A request of n query vectors (rep * its tokens) over t tiles takes
+// kv_heads * ceil(n / N) * t places, its problems one after the other, KV head slowest.
+struct Line {
+    int64_t total;
+    int32_t ctas;                        // stretches it is cut into
+};
+struct Request {
+    int32_t tokens, first_token, rows, groups, tiles;
+};
+__device__ __forceinline__ Request request_at(const Attend4Args &a, int b, int n_vec)
+{
+    Request r;
+    r.first_token = a.cu ? a.cu[b] : 0;
+    r.tokens = a.cu ? a.cu[b + 1] - r.first_token : a.n_q;
+    if (a.cu) {                          // only tokens that Q has
+        if (r.first_token < 0 || r.tokens < 0) r.tokens = 0;
+        else if ((int64_t)r.first_token + r.tokens > a.n_tokens) r.tokens = max(0, a.n_tokens - r.first_token);
+        r.tokens = min(r.tokens, a.n_q);
+    }
+    r.rows = a.idx ? a.n_kv : min(max(a.length[b], 0), a.n_kv);
+    r.groups = (r.tokens * a.rep + n_vec - 1) / n_vec;
+    r.tiles = max(1, (r.rows + A4_TILE - 1) / A4_TILE);
+    return r;
+}
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool live)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// what is left of two numbers after their rounding to fp16, as fp16
+__device__ __forceinline__ uint32_t half2_rest(float lo, float hi, uint32_t rounded)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&rounded));
+    return half2_bits(lo - f.x, hi - f.y);
+}
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <int D, int NT, int PARTS> struct A4 {
+    using R = Row4<D>;
+    static constexpr int N = 8 * NT;
+    static constexpr int KS = D / 16;                            // steps of the contraction over d
+    static constexpr int TILE_BYTES = A4_TILE * R::BYTES;
+    static constexpr int OD = D + 4;                             // floats between vectors of a warp's result (bank offset)
+    // per warp: the ring of tiles; over it, at the end of a stretch, the warp's result.  Then the rows' biases per stage, the line of tiles, Q.
+    static constexpr int WARP_BYTES = A4_STAGES * TILE_BYTES > N * OD * 4 ? A4_STAGES * TILE_BYTES : N * OD * 4;
+    static constexpr int OFF_BIAS = A4_WARPS * WARP_BYTES;
+    static constexpr int OFF_ML = OFF_BIAS + A4_WARPS * A4_STAGES * A4_TILE * 4;
+    static constexpr int OFF_QS = OFF_ML + A4_WARPS * N * 2 * 4;  // [N] scale of the logits of a vector
+    static constexpr int OFF_Q = (OFF_QS + N * 4 + 15) / 16 * 16; // [PARTS][NT][KS / 2][32 lanes] 16 bytes
+    static constexpr int OFF_LINE = OFF_Q + PARTS * NT * (KS / 2) * 512;
+    static constexpr int TOTAL = OFF_LINE + (A4_MAX_BATCH + 1) * 8;
+};
+
+// prefix[b] = places before request b; every thread returns the total
+__device__ __forceinline__ int64_t lay_line(const Attend4Args &a, int n_vec, int64_t *prefix, int64_t *part)
+{
+    int64_t before = 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int b0 = 0; b0 < a.batch; b0 += A4_THREADS) {
+        const int b = b0 + threadIdx.x;
+        int64_t mine = 0;
+        if (b < a.batch) {
+            const Request r = request_at(a, b, n_vec);
+            mine = (int64_t)a.pool.kv_heads * r.groups * r.tiles;
+        }
+        int64_t x = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) part[warp] = x;
+        __syncthreads();
+        int64_t add = before;
+        for (int i = 0; i < A4_WARPS; ++i) {
+            if (i < warp) add += part[i];
+            before += part[i];
+        }
+        if (b < a.batch) prefix[b] = add + x - mine;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) prefix[a.batch] = before;
+    __syncthreads();
+    return before;
+}
+__host__ __device__ __forceinline__ int stretches(int64_t total, int ctas)
+{
+    const int64_t most = (total + A4_CTA_TILES - 1) / A4_CTA_TILES;
+    return (int)(most < ctas ? most : ctas);
+}
+// request that place f belongs to: the last with prefix[b] <= f (requests without places are passed over)
+__device__ __forceinline__ int request_of(const int64_t *prefix, int batch, int64_t f)
+{
+    int lo = 0, hi = batch - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (prefix[mid] <= f) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+template <typename T, int D, int NT, int PARTS>
+__global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(const __grid_constant__ Attend4Args a)
+{
+    using C = A4<D, NT, PARTS>;
+    using R = Row4<D>;
+    constexpr int N = C::N, KS = C::KS;
+    constexpr int KB = D / 8, VB = D / 16;                       // bytes of codes a lane reads of a key row, of a value row
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    float *ml = reinterpret_cast<float *>(smem + C::OFF_ML);
+    float *q_scale = reinterpret_cast<float *>(smem + C::OFF_QS);
+    uint4 *q_frag = reinterpret_cast<uint4 *>(smem + C::OFF_Q);
+    int64_t *prefix = reinterpret_cast<int64_t *>(smem + C::OFF_LINE);
+    unsigned char *ring = smem + warp * C::WARP_BYTES;
+    float *bias = reinterpret_cast<float *>(smem + C::OFF_BIAS) + warp * A4_STAGES * A4_TILE;
+    const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
+
+    cudaGridDependencySynchronize();
+    const int64_t total = lay_line(a, N, prefix, reinterpret_cast<int64_t *>(smem));
+    const int ctas = stretches(total, gridDim.x);
+    if ((int)blockIdx.x >= ctas) return;
+    const int64_t begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
+    const float logit_scale = (float)(1.4426950408889634 / sqrt((double)D));
+
+    int b = request_of(prefix, a.batch, begin);
+    for (int64_t f = begin; f < end;) {
+        while (prefix[b + 1] <= f) ++b;
+        const Request rq = request_at(a, b, N);
+        const int64_t in_request = f - prefix[b];
+        const int problem = (int)(in_request / rq.tiles), tile0 = (int)(in_request - (int64_t)problem * rq.tiles);
+        const int tile1 = (int)min((int64_t)rq.tiles, tile0 + (end - f));
+        const int h = problem / rq.groups, group = problem - h * rq.groups;
+        const bool whole = tile0 == 0 && tile1 == rq.tiles;
+        const bool first_segment = f == begin;
+        f += tile1 - tile0;
+        const int vec0 = group * N;                              // vector v of the group is token (vec0 + v) / rep, head h rep + (vec0 + v) % rep
+        const int vectors = min(N, rq.tokens * a.rep - vec0);
+        // rows a vector sees: the last token all of them, the one before it one less
+        const bool tail = a.causal && !a.idx;
+        const int last_seen = tail ? rq.rows - rq.tokens + 1 + (vec0 + vectors - 1) / a.rep : rq.rows;
+        const int first_seen = tail ? rq.rows - rq.tokens + 1 + vec0 / a.rep : rq.rows;
+        const int tile_end = min(tile1, (last_seen + A4_TILE - 1) / A4_TILE);
+
+        // ---- the rows of this warp's tiles: lane i has row i of the tile ----
+        uint32_t next_row = NO_ROW;
+        float next_bias = -INFINITY;
+        auto look_up = [&](int tile) {
+            next_row = NO_ROW;
+            next_bias = -INFINITY;
+            const int e = tile * A4_TILE + lane;
+            if (tile < tile_end && e < rq.rows) {
+                int64_t r = e;
+                float lw = 0.f;
+                if (a.idx) {
+                    const int64_t at = ((int64_t)b * a.pool.kv_heads + h) * a.n_kv + e;
+                    const float w = a.w[at];
+                    r = w > 0.f ? a.idx[at] : -1;
+                    lw = log2f(w);
+                }
+                next_row = pool_row(a.pool, b, h, r);
+                if (next_row != NO_ROW) next_bias = lw;
+            }
+        };
+        auto fetch = [&](int stage, bool any) {
+            if (any) {
+                bias[stage * A4_TILE + lane] = next_bias;
+                const uint32_t dst = ring_u32 + stage * C::TILE_BYTES;
+#pragma unroll
+                for (int i = 0; i < R::CHUNKS; ++i) {
+                    const int c = i * 32 + lane, row = c / R::CHUNKS, chunk = c - row * R::CHUNKS;
+                    const uint32_t from = __shfl_sync(0xffffffffu, next_row, row);
+                    // (a row that is not there is filled with zeros: codes and scales of 0)
+                    cp16(dst + c * 16, a.pool.rows + (from != NO_ROW ? (uint64_t)from * R::BYTES + chunk * 16 : 0), from != NO_ROW);
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        int ahead = tile0 + warp;
+        look_up(ahead);
+#pragma unroll
+        for (int s = 0; s < A4_STAGES - 1; ++s) {
+            fetch(s, ahead < tile_end);
+            ahead += A4_WARPS;
+            look_up(ahead);
+        }
+
+        // ---- queries: vector v by the threads of a 16th of the CTA; scaled by a power of two, laid out as the lanes want them ----
+        {
+            constexpr int PER = A4_THREADS / N, EACH = D / PER;  // threads to a vector, numbers to a thread
+            const int v = threadIdx.x / PER, sub = threadIdx.x % PER;
+            const int vv = vec0 + v, tok = vv / a.rep, head = h * a.rep + vv % a.rep;
+            float x[EACH];
+            float top = 0.f;
+            if (v < vectors) {
+                const T *src = (const T *)a.q + (a.cu ? (int64_t)(rq.first_token + tok) * a.qs[2] : b * a.qs[0] + tok * a.qs[2]) + head * a.qs[1];
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) {
+                    x[i] = load_as<float>(src, sub * EACH + i);
+                    top = fmaxf(top, fabsf(x[i]));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) x[i] = 0.f;
+            }
+#pragma unroll
+            for (int o = PER / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            // 2^(11 - e) with e the exponent of the largest (of a subnormal one: that of the smallest normal number)
+            int e = (int)(__float_as_uint(top) >> 23) - 127;
+            e = top == 0.f ? 11 : max(-126, min(127, e));
+            const float up = e > 11 - 127 ? ldexpf(1.f, 11 - e) : 0x1p127f;
+            if (sub == 0) q_scale[v] = logit_scale / up;
+            // lane (v % 8, lane_t) of tile v / 8 has numbers [D / 4 lane_t, D / 4 (lane_t + 1)), a step of the contraction four of them
+#pragma unroll
+            for (int i = 0; i < EACH; i += 2) {
+                const int n = sub * EACH + i, lane_t = n / (D / 4), in = n % (D / 4);
+                const int step = in / 4, pair = (in / 2) % 2;
+                uint32_t hi = half2_bits(x[i] * up, x[i + 1] * up);
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    uint32_t *to = reinterpret_cast<uint32_t *>(q_frag + ((p * NT + v / 8) * (KS / 2) + step / 2) * 32 + (v % 8) * 4 + lane_t);
+                    to[(step % 2) * 2 + pair] = hi;
+                    if (p + 1 < PARTS) hi = half2_rest(x[i] * up, x[i + 1] * up, hi);
+                }
+            }
+        }
+        __syncthreads();
+
+        // ---- the warp's tiles ----
+        float o[NT][KS][4], l[NT][2], ref[NT][2], qs[NT][2];
+        int seen[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int v = n * 8 + 2 * t + x;
+                l[n][x] = 0.f;
+                ref[n][x] = -INFINITY;
+                qs[n][x] = q_scale[v];
+                seen[n][x] = tail ? rq.rows - rq.tokens + 1 + (vec0 + v) / a.rep : rq.rows;
+            }
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[n][i][x] = 0.f;
+        }
+        int stage = 0;
+        for (int tile = tile0 + warp; tile < tile_end; tile += A4_WARPS) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(A4_STAGES - 2) : "memory");
+            __syncwarp();
+            const unsigned char *rows = ring + stage * C::TILE_BYTES;
+            const float *rb = bias + stage * A4_TILE;
+            {
+                // the stage read in the last round is free
+                const int to = stage + A4_STAGES - 1;
+                fetch(to >= A4_STAGES ? to - A4_STAGES : to, ahead < tile_end);
+                ahead += A4_WARPS;
+                look_up(ahead);
+            }
+            stage = stage + 1 == A4_STAGES ? 0 : stage + 1;
+
+            const bool cut = (tile + 1) * A4_TILE > first_seen;
+            // a value that is NaN must not reach a vector that does not see its row through 0 x NaN: such scales are taken out here and put
+            // back as NaN sums of those that see it
+            uint32_t nan_groups = 0, nan_rows = 0;
+            if (cut) {
+                unsigned char *vscale = ring + (rows - ring) + lane * R::BYTES + R::SCALES + R::GROUPS;
+#pragma unroll
+                for (int i = 0; i < R::GROUPS; ++i)
+                    if (vscale[i] >= 0xf8u) {
+                        nan_groups |= 1u << i;
+                        vscale[i] = 0;
+                    }
+                nan_rows = __ballot_sync(0xffffffffu, nan_groups != 0);
+                __syncwarp();
+            }
+
+            // ---- logits: s[block of 16 rows][tile of vectors] = rows g, g + 8 x vectors 2t, 2t + 1 ----
+            float s[2][NT][4];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                uint32_t codes[2][KB / 4], scale[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const unsigned char *row = rows + (kb * 16 + x * 8 + g) * R::BYTES;
+                    if constexpr (D == 128) {
+                        const uint4 c = *reinterpret_cast<const uint4 *>(row + t * KB);
+                        codes[x][0] = c.x; codes[x][1] = c.y; codes[x][2] = c.z; codes[x][3] = c.w;
+                        scale[x] = *reinterpret_cast<const unsigned short *>(row + R::SCALES + 2 * t);
+                    } else {
+                        const uint2 c = *reinterpret_cast<const uint2 *>(row + t * KB);
+                        codes[x][0] = c.x; codes[x][1] = c.y;
+                        scale[x] = row[R::SCALES + t];
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) s[kb][n][x] = 0.f;
+#pragma unroll
+                for (int w = 0; w < KB / 4; ++w) {               // a word: eight numbers, two steps
+                    uint32_t half[2][4];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        codes8_to_half2(codes[x][w], half[x]);
+                        const uint32_t sc = scale4_half_bits(D == 128 && w >= 2 ? scale[x] >> 8 : scale[x] & 0xffu) * 0x10001u;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) half[x][i] = hmul2_bits(half[x][i], sc);
+                    }
+                    const uint32_t a0[4] = {half[0][0], half[1][0], half[0][1], half[1][1]};
+                    const uint32_t a1[4] = {half[0][2], half[1][2], half[0][3], half[1][3]};
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        if constexpr (PARTS == 1) {
+                            const uint4 q = q_frag[(n * (KS / 2) + w) * 32 + lane];
+                            mma_f16(s[kb][n], a0, q.x, q.y);
+                            mma_f16(s[kb][n], a1, q.z, q.w);
+                        } else {
+                            // a chain of four, the small parts first
+                            float c[4] = {0.f, 0.f, 0.f, 0.f};
+                            const uint4 lo = q_frag[((NT + n) * (KS / 2) + w) * 32 + lane], hi = q_frag[(n * (KS / 2) + w) * 32 + lane];
+                            mma_f16(c, a0, lo.x, lo.y);
+                            mma_f16(c, a1, lo.z, lo.w);
+                            mma_f16(c, a0, hi.x, hi.y);
+                            mma_f16(c, a1, hi.z, hi.w);
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) s[kb][n][x] += c[x];
+                        }
+                    }
+                }
+            }
+
+            // ---- logits in base 2 with the weights; what is not seen is -inf whatever it holds ----
+            float top[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int at = kb * 16 + x * 8 + g;
+                    const float lw = rb[at];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            float &z = s[kb][n][2 * x + y];
+                            z = fmaf(z, qs[n][y], lw);
+                            if (lw == -INFINITY || (cut && tile * A4_TILE + at >= seen[n][y])) z = -INFINITY;
+                            top[n][y] = fmaxf(top[n][y], z);
+                        }
+                }
+            bool moved = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                    for (int off = 4; off < 32; off <<= 1) top[n][y] = fmaxf(top[n][y], __shfl_xor_sync(0xffffffffu, top[n][y], off));
+                    moved |= top[n][y] > ref[n][y] + A4_SLACK;   // (the first rows seen, too: ref is -inf)
+                }
+            if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const float to = fmaxf(ref[n][y], top[n][y]);
+                        const float f2 = ref[n][y] == -INFINITY ? 0.f : exp2_fast(ref[n][y] - to);
+                        ref[n][y] = to;
+                        l[n][y] *= f2;
+#pragma unroll
+                        for (int i = 0; i < KS; ++i) {
+                            o[n][i][y] *= f2;
+                            o[n][i][2 + y] *= f2;
+                        }
+                    }
+            }
+            // ---- probabilities: the P operand of rows [16 kb, 16 kb + 16) ----
+            uint32_t pb[PARTS][2][NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float r0 = ref[n][0] == -INFINITY ? 0.f : ref[n][0] - A4_LIFT, r1 = ref[n][1] == -INFINITY ? 0.f : ref[n][1] - A4_LIFT;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const float p0 = exp2_fast(s[kb][n][2 * x] - r0), p1 = exp2_fast(s[kb][n][2 * x + 1] - r1);
+                        l[n][0] += p0;
+                        l[n][1] += p1;
+                        const uint32_t hi = half2_bits(p0, p1);
+                        pb[0][kb][n][x] = transpose8x8(hi);
+                        if constexpr (PARTS == 2) pb[1][kb][n][x] = transpose8x8(half2_rest(p0, p1, hi));
+                    }
+            }
+            // ---- O^T += V^T P^T: lane row g of step i has numbers D / 8 g + 2 i and, 8 rows on, + 2 i + 1 ----
+            uint32_t vw[2][2][2][VB / 4], vs[2][2];              // [block][rows 2t, 2t + 8][row, next row][word]
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const unsigned char *row = rows + (kb * 16 + x * 8 + 2 * t) * R::BYTES;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        if constexpr (D == 128) {
+                            const uint2 c = *reinterpret_cast<const uint2 *>(row + y * R::BYTES + R::CODES + g * VB);
+                            vw[kb][x][y][0] = c.x;
+                            vw[kb][x][y][1] = c.y;
+                        } else {
+                            vw[kb][x][y][0] = *reinterpret_cast<const uint32_t *>(row + y * R::BYTES + R::CODES + g * VB);
+                        }
+                    }
+                    const int sg = R::SCALES + R::GROUPS + (D == 128 ? g : g / 2);
+                    vs[kb][x] = scale4_half_bits(row[sg]) | (scale4_half_bits(row[R::BYTES + sg]) << 16);
+                }
+#pragma unroll
+            for (int w = 0; w < VB / 4; ++w) {
+                uint32_t even[2][2][4], odd[2][2][4];            // numbers 2 i and 2 i + 1 of rows (2t, 2t + 1), i = 4 w ..
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const uint32_t r0 = vw[kb][x][0][w], r1 = vw[kb][x][1][w];
+                        codes8_to_half2((r0 & 0x0f0f0f0fu) | ((r1 << 4) & 0xf0f0f0f0u), even[kb][x]);
+                        codes8_to_half2(((r0 >> 4) & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u), odd[kb][x]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            even[kb][x][i] = hmul2_bits(even[kb][x][i], vs[kb][x]);
+                            odd[kb][x][i] = hmul2_bits(odd[kb][x][i], vs[kb][x]);
+                        }
+                    }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t a0[4] = {even[0][0][i], odd[0][0][i], even[0][1][i], odd[0][1][i]};
+                    const uint32_t a1[4] = {even[1][0][i], odd[1][0][i], even[1][1][i], odd[1][1][i]};
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float(&acc)[4] = o[n][4 * w + i];
+                        if constexpr (PARTS == 1) {
+                            mma_f16(acc, a0, pb[0][0][n][0], pb[0][0][n][1]);
+                            mma_f16(acc, a1, pb[0][1][n][0], pb[0][1][n][1]);
+                        } else {
+                            float c[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma_f16(c, a0, pb[1][0][n][0], pb[1][0][n][1]);
+                            mma_f16(c, a1, pb[1][1][n][0], pb[1][1][n][1]);
+                            mma_f16(c, a0, pb[0][0][n][0], pb[0][0][n][1]);
+                            mma_f16(c, a1, pb[0][1][n][0], pb[0][1][n][1]);
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) acc[x] += c[x];
+                        }
+                    }
+                }
+            }
+            while (nan_rows) {
+                const int row = __ffs(nan_rows) - 1;
+                nan_rows &= nan_rows - 1;
+                const uint32_t groups = __shfl_sync(0xffffffffu, nan_groups, row);
+                if ((groups >> (D == 128 ? g : g / 2)) & 1u)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+                            if (tile * A4_TILE + row < seen[n][y])
+#pragma unroll
+                                for (int i = 0; i < KS; ++i) o[n][i][y] = o[n][i][2 + y] = __int_as_float(0x7fffffff);
+            }
+            __syncwarp();                                        // (the next round overwrites this stage)
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+
+        // ---- the warps' results, joined in the order of the warps ----
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) l[n][y] += __shfl_xor_sync(0xffffffffu, l[n][y], off);
+                // (a maximum passes over NaN: a vector all of whose logits are NaN has seen something, too)
+                if (ref[n][y] == -INFINITY && l[n][y] != 0.f) ref[n][y] = 0.f;
+                const int v = n * 8 + 2 * t + y;
+                if (g == 0) {
+                    ml[(warp * N + v) * 2] = ref[n][y];
+                    ml[(warp * N + v) * 2 + 1] = l[n][y];
+                }
+                float *to = reinterpret_cast<float *>(ring) + v * C::OD + g * (D / 8);
+#pragma unroll
+                for (int i = 0; i < KS; i += 2)
+                    *reinterpret_cast<float4 *>(to + 2 * i) = make_float4(o[n][i][y], o[n][i][2 + y], o[n][i + 1][y], o[n][i + 1][2 + y]);
+            }
+        }
+        __syncthreads();
+        {
+            constexpr int PER = A4_THREADS / N, EACH = D / PER;
+            const int v = threadIdx.x / PER, sub = threadIdx.x % PER;
+            float m = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < A4_WARPS; ++i) m = fmaxf(m, ml[(i * N + v) * 2]);
+            float den = 0.f, acc[EACH];
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) acc[e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < A4_WARPS; ++i) {
+                const float mi = ml[(i * N + v) * 2];
+                if (mi == -INFINITY) continue;                   // (has seen nothing)
+                const float share = exp2_fast(mi - m);
+                den = fmaf(ml[(i * N + v) * 2 + 1], share, den);
+                const float *from = reinterpret_cast<const float *>(smem + i * C::WARP_BYTES) + v * C::OD;
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) acc[e] = fmaf(from[sub + e * PER], share, acc[e]);
+            }
+            if (whole) {
+                if (v < vectors) {
+                    const int vv = vec0 + v, tok = vv / a.rep, head = h * a.rep + vv % a.rep;
+                    T *to = (T *)a.o + (a.cu ? (int64_t)(rq.first_token + tok) * a.os[2] : b * a.os[0] + tok * a.os[2]) + head * a.os[1];
+                    const float inv = m == -INFINITY ? 0.f : 1.f / den;
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e) store_from(to, sub + e * PER, acc[e] * inv);
+                }
+            } else {
+                float *to = a.part + ((int64_t)(2 * blockIdx.x + (first_segment ? 0 : 1)) * N + v) * (D + 2);
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) to[sub + e * PER] = acc[e];
+                if (sub == 0) {
+                    to[D] = m;
+                    to[D + 1] = den;
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// A CTA per problem (request, KV head, group): joins the parts of the stretches that share it, in their order.
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(A4_THREADS) attend4_merge_kernel(const __grid_constant__ Attend4Args a, int ctas_launched, int max_groups)
+{
+    constexpr int N = 8 * NT;
+    constexpr int PER = A4_THREADS / N, EACH = D / PER;
+    __shared__ int64_t prefix[A4_MAX_BATCH + 1], part[A4_WARPS];
+    cudaGridDependencySynchronize();
+    const int64_t total = lay_line(a, N, prefix, part);
+    const int ctas = stretches(total, ctas_launched);
+    const int b = blockIdx.x / (a.pool.kv_heads * max_groups), rest = blockIdx.x % (a.pool.kv_heads * max_groups);
+    const int h = rest / max_groups, group = rest % max_groups;
+    const Request rq = request_at(a, b, N);
+    if (group >= rq.groups) return;
+    const int64_t f0 = prefix[b] + (int64_t)(h * rq.groups + group) * rq.tiles, f1 = f0 + rq.tiles;
+    // stretch c is [total c / ctas, total (c + 1) / ctas): the one that place f is in
+    const int64_t c0 = ((f0 + 1) * ctas - 1) / total, c1 = (f1 * ctas - 1) / total;
+    if (c0 == c1) return;
+    const int v = threadIdx.x / PER, sub = threadIdx.x % PER;
+    auto slot = [&](int64_t c) {
+        const bool first = c > c0 || total * c / ctas == f0;     // the stretch begins with this problem
+        return a.part + ((2 * c + (first ? 0 : 1)) * N + v) * (D + 2);
+    };
+    float m = -INFINITY;
+    for (int64_t c = c0; c <= c1; ++c) m = fmaxf(m, slot(c)[D]);
+    float den = 0.f, acc[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) acc[e] = 0.f;
+    for (int64_t c = c0; c <= c1; ++c) {
+        const float *from = slot(c);
+        if (from[D] == -INFINITY) continue;
+        const float share = exp2_fast(from[D] - m);
+        den = fmaf(from[D + 1], share, den);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) acc[e] = fmaf(from[sub + e * PER], share, acc[e]);
+    }
+    const int vec0 = group * N;
+    if (v >= rq.tokens * a.rep - vec0) return;
+    const int vv = vec0 + v, tok = vv / a.rep, head = h * a.rep + vv % a.rep;
+    T *to = (T *)a.o + (a.cu ? (int64_t)(rq.first_token + tok) * a.os[2] : b * a.os[0] + tok * a.os[2]) + head * a.os[1];
+    const float inv = m == -INFINITY ? 0.f : 1.f / den;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) store_from(to, sub + e * PER, acc[e] * inv);
+}
+
+template <typename T, int D, int NT, int PARTS> int attend4_ctas(int *out)
+{
+    using C = A4<D, NT, PARTS>;
+    auto kern = attend4_kernel<T, D, NT, PARTS>;
+    ELM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::TOTAL));
+    int per_sm = 0;
+    ELM_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, A4_THREADS, C::TOTAL));
+    *out = (per_sm < 1 ? 1 : per_sm) * device_sm_count();
+    return ELM_OK;
+}
+constexpr int A4_MAX_CTAS_PER_SM = 8;    // what the workspace has room for
+
+template <typename T, int D, int NT, int PARTS> int launch_attend4(const Attend4Args &a, cudaStream_t st)
+{
+    using C = A4<D, NT, PARTS>;
+    int ctas = 0;
+    const int rc = attend4_ctas<T, D, NT, PARTS>(&ctas);
+    if (rc != ELM_OK) return rc;
+    const int most = A4_MAX_CTAS_PER_SM * device_sm_count();
+    if (ctas > most) ctas = most;
+    const int max_groups = (int)(((int64_t)a.n_q * a.rep + C::N - 1) / C::N);
+    const int64_t problems = (int64_t)a.batch * a.pool.kv_heads * max_groups;
+    if (problems > 0x7fffffff) return ELM_ERR_SHAPE;
+    // no more CTAs than the longest line of tiles has stretches
+    const int64_t places = problems * ((a.n_kv + A4_TILE - 1) / A4_TILE);
+    const int grid = stretches(places, ctas);
+    ELM_CUDA_TRY(launch_after(attend4_kernel<T, D, NT, PARTS>, dim3((unsigned)grid), dim3(A4_THREADS), C::TOTAL, st, a));
+    ELM_CUDA_TRY(launch_after(attend4_merge_kernel<T, D, NT>, dim3((unsigned)problems), dim3(A4_THREADS), 0, st, a, grid, max_groups));
+    count_launches(2);
+    return cuda_status(cudaGetLastError());
+}
+
+bool zeros(const int64_t (&s)[3]) { return s[0] == 0 && s[1] == 0 && s[2] == 0; }
+
+int check(const elm_cache4_params *p, bool list, int &shift, int64_t &n_kv)
+{
+    if (p->dtype != ELM_F32 && p->dtype != ELM_BF16) return ELM_ERR_DTYPE;
+    if (p->batch < 1 || p->batch > A4_MAX_BATCH || p->kv_heads < 1 || p->q_heads < 1 || p->q_heads % p->kv_heads != 0) return ELM_ERR_SHAPE;
+    if ((int64_t)p->batch * p->q_heads > 65535 || (p->d != 64 && p->d != 128)) return ELM_ERR_SHAPE;
+    if (p->n_q < 1 || p->n_tokens < 0 || p->n_kv < 0 || (list && p->n_kv < 1) || p->max_pages < 1) return ELM_ERR_SHAPE;
+    shift = page_shift_of(p->page_rows);
+    if (shift < 0 || !pool_fits(p->n_pages, p->page_rows, p->kv_heads)) return ELM_ERR_SHAPE;
+    const int64_t capacity = (int64_t)p->max_pages << shift;
+    if (capacity > 0x7fffffff - 64) return ELM_ERR_SHAPE;
+    n_kv = list ? p->n_kv : (p->n_kv == 0 || p->n_kv > capacity ? capacity : p->n_kv);
+    if (n_kv > 0x7fffffff - 64 || (int64_t)p->n_q * (p->q_heads / p->kv_heads) > 0x7fffffff / 2) return ELM_ERR_SHAPE;
+    return ELM_OK;
+}
+
+// Lists met by so many queries that the tensor-core kernel of elm_attend, 256 queries of a head at a time, is the faster way.
+bool by_tensor_cores(const elm_cache4_params *p, bool list)
+{
+    if (!list || p->dtype != ELM_BF16 || !zeros(p->q_stride) || !zeros(p->o_stride)) return false;
+    return p->n_q >= 128;
+}
+
+elm_params as_attend(const elm_cache4_params *p)
+{
+    elm_params e = {};
+    e.batch = p->batch;
+    e.q_heads = p->q_heads;
+    e.kv_heads = p->kv_heads;
+    e.n_kv = p->n_kv;
+    e.n_q = p->n_q;
+    e.d = p->d;
+    e.dtype = ELM_BF16;
+    e.precision = ELM_PREC_FP32;
+    e.delta = 0.5;
+    return e;
+}
+
+size_t workspace_of(const elm_cache4_params *p, bool list)
+{
+    if (by_tensor_cores(p, list)) {
+        const elm_params e = as_attend(p);
+        return attend_layout(&e, p->n_kv).total;
+    }
+    const int vectors = (int64_t)p->n_q * (p->q_heads / p->kv_heads) <= 8 ? 8 : 16;
+    return (size_t)2 * A4_MAX_CTAS_PER_SM * device_sm_count() * vectors * (p->d + 2) * sizeof(float);
+}
+
+}  // namespace
+}  // namespace elm
+
+using namespace elm;
+
+extern "C" int elm_cache4_attend_workspace_bytes(const elm_cache4_params *p, int32_t with_list, size_t *bytes)
+{
+    if (!p || !bytes) return ELM_ERR_NULL;
+    int shift;
+    int64_t n_kv;
+    const int rc = check(p, with_list != 0, shift, n_kv);
+    if (rc != ELM_OK) return rc;
+    *bytes = workspace_of(p, with_list != 0);
+    return ELM_OK;
+}
+
+extern "C" int elm_cache4_attend(const void *Q, const void *rows, const int32_t *table, const int32_t *length, const int32_t *cu,
+                                 const int32_t *idx, const float *w, const elm_cache4_params *p, void *O, void *workspace,
+                                 size_t workspace_bytes, void *stream)
+{
+    if (!p) return ELM_ERR_NULL;
+    const bool list = idx != nullptr;
+    int shift;
+    int64_t n_kv;
+    const int rc = check(p, list, shift, n_kv);
+    if (rc != ELM_OK) return rc;
+    if (!Q || !rows || !table || !O || !workspace || (list ? !w : !length)) return ELM_ERR_NULL;
+    if (list && (length || cu)) return ELM_ERR_SHAPE;                       // exactly one of the two forms
+    if (((uintptr_t)Q | (uintptr_t)O | (uintptr_t)rows) & 15 || ((uintptr_t)workspace & 255)) return ELM_ERR_ALIGN;
+    if (((uintptr_t)table | (uintptr_t)length | (uintptr_t)cu | (uintptr_t)idx | (uintptr_t)w) & 3) return ELM_ERR_ALIGN;
+    if (workspace_bytes < workspace_of(p, list)) return ELM_ERR_WORKSPACE;
+    cudaStream_t st = (cudaStream_t)stream;
+    Attend4Args a = {};
+    a.pool = Pool4{(const unsigned char *)rows, table, p->n_pages, p->max_pages, shift, p->kv_heads};
+    if (by_tensor_cores(p, list)) {
+        const elm_params e = as_attend(p);
+        AttendWindow win;
+        win.pool4 = &a.pool;
+        return attend_tc((const __nv_bfloat16 *)Q, nullptr, nullptr, idx, w, p->n_kv, &e, (__nv_bfloat16 *)O, (unsigned char *)workspace, st, true, win);
+    }
+    a.q = Q;
+    a.o = O;
+    a.length = length;
+    a.cu = cu;
+    a.idx = idx;
+    a.w = w;
+    a.part = (float *)workspace;
+    const int64_t d = p->d, heads = p->q_heads;
+    const int64_t dense[3] = {heads * p->n_q * d, cu ? d : p->n_q * d, cu ? heads * d : d};
+    for (int i = 0; i < 3; ++i) {
+        a.qs[i] = zeros(p->q_stride) ? dense[i] : p->q_stride[i];
+        a.os[i] = zeros(p->o_stride) ? dense[i] : p->o_stride[i];
+    }
+    // rows of O that would be written twice
+    if ((!cu && p->batch > 1 && a.os[0] == 0) || (p->q_heads > 1 && a.os[1] == 0) || ((cu ? p->n_tokens : p->n_q) > 1 && a.os[2] == 0)) return ELM_ERR_SHAPE;
+    a.batch = p->batch;
+    a.q_heads = p->q_heads;
+    a.rep = p->q_heads / p->kv_heads;
+    a.n_kv = (int32_t)n_kv;
+    a.n_q = p->n_q;
+    a.n_tokens = p->n_tokens;
+    a.causal = p->causal;
+    const bool few = (int64_t)p->n_q * a.rep <= 8;
+    typedef __nv_bfloat16 bf;
+    if (p->dtype == ELM_BF16) {
+        if (p->d == 64) return few ? launch_attend4<bf, 64, 1, 1>(a, st) : launch_attend4<bf, 64, 2, 1>(a, st);
+        return few ? launch_attend4<bf, 128, 1, 1>(a, st) : launch_attend4<bf, 128, 2, 1>(a, st);
+    }
+    if (p->d == 64) return few ? launch_attend4<float, 64, 1, 2>(a, st) : launch_attend4<float, 64, 2, 2>(a, st);
+    return few ? launch_attend4<float, 128, 1, 2>(a, st) : launch_attend4<float, 128, 2, 2>(a, st);
+}
+
+extern "C" int elm_cache4_attend_status(const void *workspace, const elm_cache4_params *p, int32_t with_list, int32_t *status_host, void *stream)
+{
+    if (!workspace || !p || !status_host) return ELM_ERR_NULL;
+    int shift;
+    int64_t n_kv;
+    const int rc = check(p, with_list != 0, shift, n_kv);
+    if (rc != ELM_OK) return rc;
+    if (by_tensor_cores(p, with_list != 0)) {
+        const elm_params e = as_attend(p);
+        return elm_attend_status(workspace, &e, p->n_kv, status_host, stream);
+    }
+    ELM_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
+    *status_host = 0;                                                       // (nothing waits in that form)
+    return ELM_OK;
+}
