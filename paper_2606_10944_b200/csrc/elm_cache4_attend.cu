@@ -30,9 +30,10 @@ namespace {
 constexpr int A4_WARPS = 4;
 constexpr int A4_THREADS = 32 * A4_WARPS;
 constexpr int A4_TILE = 32;              // rows of a warp's tile
-constexpr int A4_STAGES = 3;
+constexpr int A4_STAGES = 2;
+constexpr int A4_START = 8;              // what a problem's beginning and end cost, in tiles
 constexpr int A4_MAX_BATCH = 1024;
-constexpr int A4_CTA_TILES = A4_WARPS;   // a CTA's stretch holds at least these
+constexpr int A4_CTA_PLACES = A4_START / 2 + A4_WARPS;     // a CTA's stretch holds at least these
 constexpr float A4_LIFT = 8.f;           // probabilities are 2^8 times their share of the reference's
 constexpr float A4_SLACK = 6.f;          // how far the maximum may pass the reference: fp16 ends at 2^16
 
@@ -42,19 +43,17 @@ struct Attend4Args {
     void *o;
     const int32_t *length, *cu, *idx;
     const float *w;
-    float *part;                         // [2 * ctas][N][D + 2]
+    float *part;                         // sums [2 * ctas][N][D], then (reference, denominator) [2 * ctas][N]
     int64_t qs[3], os[3];
     int32_t batch, q_heads, rep, n_kv, n_q, n_tokens, causal;
 };
 
-// Where the problems of every request begin in the line of tiles.  A request of n query vectors (rep * its tokens) over t tiles takes
-// kv_heads * ceil(n / N) * t places, its problems one after the other, KV head slowest.
-struct Line {
-    int64_t total;
-    int32_t ctas;                        // stretches it is cut into
-};
+// Where the problems of every request begin in the line of tiles.  A request of n query vectors (rep * its tokens) over t tiles has
+// kv_heads * ceil(n / N) problems of A4_START + t places each, one after the other, KV head slowest.  The first A4_START places of a problem hold no
+// tile: they stand for what it costs whatever its length (48 requests of 1 .. 32768 rows, lengths spread over the logarithm: the CTAs that
+// met many short ones took 2.5 times as long as the others).
 struct Request {
-    int32_t tokens, first_token, rows, groups, tiles;
+    int32_t tokens, first_token, rows, groups, tiles, places;
 };
 __device__ __forceinline__ Request request_at(const Attend4Args &a, int b, int n_vec)
 {
@@ -69,6 +68,7 @@ __device__ __forceinline__ Request request_at(const Attend4Args &a, int b, int n
     r.rows = a.idx ? a.n_kv : min(max(a.length[b], 0), a.n_kv);
     r.groups = (r.tokens * a.rep + n_vec - 1) / n_vec;
     r.tiles = max(1, (r.rows + A4_TILE - 1) / A4_TILE);
+    r.places = A4_START + r.tiles;
     return r;
 }
 
@@ -119,7 +119,7 @@ template <int D, int NT, int PARTS> struct A4 {
     static constexpr int OFF_QS = OFF_ML + A4_WARPS * N * 2 * 4;  // [N] scale of the logits of a vector
     static constexpr int OFF_Q = (OFF_QS + N * 4 + 15) / 16 * 16; // [PARTS][NT][KS / 2][32 lanes] 16 bytes
     static constexpr int OFF_LINE = OFF_Q + PARTS * NT * (KS / 2) * 512;
-    static constexpr int TOTAL = OFF_LINE + (A4_MAX_BATCH + 1) * 8;
+    static int total(int batch) { return OFF_LINE + (batch + 1) * 8; }
 };
 
 // prefix[b] = places before request b; every thread returns the total
@@ -127,12 +127,12 @@ __device__ __forceinline__ int64_t lay_line(const Attend4Args &a, int n_vec, int
 {
     int64_t before = 0;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int b0 = 0; b0 < a.batch; b0 += A4_THREADS) {
+    for (int b0 = 0; b0 < a.batch; b0 += blockDim.x) {
         const int b = b0 + threadIdx.x;
         int64_t mine = 0;
         if (b < a.batch) {
             const Request r = request_at(a, b, n_vec);
-            mine = (int64_t)a.pool.kv_heads * r.groups * r.tiles;
+            mine = (int64_t)a.pool.kv_heads * r.groups * r.places;
         }
         int64_t x = mine;
 #pragma unroll
@@ -143,7 +143,7 @@ __device__ __forceinline__ int64_t lay_line(const Attend4Args &a, int n_vec, int
         if (lane == 31) part[warp] = x;
         __syncthreads();
         int64_t add = before;
-        for (int i = 0; i < A4_WARPS; ++i) {
+        for (int i = 0; i < (int)(blockDim.x >> 5); ++i) {
             if (i < warp) add += part[i];
             before += part[i];
         }
@@ -156,7 +156,7 @@ __device__ __forceinline__ int64_t lay_line(const Attend4Args &a, int n_vec, int
 }
 __host__ __device__ __forceinline__ int stretches(int64_t total, int ctas)
 {
-    const int64_t most = (total + A4_CTA_TILES - 1) / A4_CTA_TILES;
+    const int64_t most = (total + A4_CTA_PLACES - 1) / A4_CTA_PLACES;
     return (int)(most < ctas ? most : ctas);
 }
 // request that place f belongs to: the last with prefix[b] <= f (requests without places are passed over)
@@ -171,7 +171,8 @@ __device__ __forceinline__ int request_of(const int64_t *prefix, int batch, int6
     return lo;
 }
 
-template <typename T, int D, int NT, int PARTS>
+// LIST: entries idx with weights w, looked up row by row; else a request's rows, in pages of at least 16: half a tile lies in one page.
+template <typename T, int D, int NT, int PARTS, bool LIST>
 __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(const __grid_constant__ Attend4Args a)
 {
     using C = A4<D, NT, PARTS>;
@@ -200,50 +201,71 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
         while (prefix[b + 1] <= f) ++b;
         const Request rq = request_at(a, b, N);
         const int64_t in_request = f - prefix[b];
-        const int problem = (int)(in_request / rq.tiles), tile0 = (int)(in_request - (int64_t)problem * rq.tiles);
-        const int tile1 = (int)min((int64_t)rq.tiles, tile0 + (end - f));
+        const int problem = (int)(in_request / rq.places), place0 = (int)(in_request - (int64_t)problem * rq.places);
+        const int place1 = (int)min((int64_t)rq.places, place0 + (end - f));
+        const bool first_segment = f == begin;
+        f += place1 - place0;
+        const int tile0 = max(0, place0 - A4_START), tile1 = place1 - A4_START;
+        if (tile1 <= tile0) continue;                            // (only what stands for a problem's beginning)
         const int h = problem / rq.groups, group = problem - h * rq.groups;
         const bool whole = tile0 == 0 && tile1 == rq.tiles;
-        const bool first_segment = f == begin;
-        f += tile1 - tile0;
         const int vec0 = group * N;                              // vector v of the group is token (vec0 + v) / rep, head h rep + (vec0 + v) % rep
         const int vectors = min(N, rq.tokens * a.rep - vec0);
         // rows a vector sees: the last token all of them, the one before it one less
-        const bool tail = a.causal && !a.idx;
+        const bool tail = !LIST && a.causal;
         const int last_seen = tail ? rq.rows - rq.tokens + 1 + (vec0 + vectors - 1) / a.rep : rq.rows;
         const int first_seen = tail ? rq.rows - rq.tokens + 1 + vec0 / a.rep : rq.rows;
         const int tile_end = min(tile1, (last_seen + A4_TILE - 1) / A4_TILE);
 
-        // ---- the rows of this warp's tiles: lane i has row i of the tile ----
-        uint32_t next_row = NO_ROW;
+        // ---- the rows of this warp's tiles, looked up a tile before they are fetched ----
+        uint32_t next_row[2] = {NO_ROW, NO_ROW};                 // LIST: [0] is lane's row of the tile; else the first rows of its halves
         float next_bias = -INFINITY;
         auto look_up = [&](int tile) {
-            next_row = NO_ROW;
+            next_row[0] = next_row[1] = NO_ROW;
             next_bias = -INFINITY;
-            const int e = tile * A4_TILE + lane;
-            if (tile < tile_end && e < rq.rows) {
-                int64_t r = e;
-                float lw = 0.f;
-                if (a.idx) {
+            if (tile >= tile_end) return;
+            if constexpr (LIST) {
+                const int e = tile * A4_TILE + lane;
+                if (e < rq.rows) {
                     const int64_t at = ((int64_t)b * a.pool.kv_heads + h) * a.n_kv + e;
                     const float w = a.w[at];
-                    r = w > 0.f ? a.idx[at] : -1;
-                    lw = log2f(w);
+                    if (w > 0.f) next_row[0] = pool_row(a.pool, b, h, a.idx[at]);
+                    if (next_row[0] != NO_ROW) next_bias = log2f(w);
                 }
-                next_row = pool_row(a.pool, b, h, r);
-                if (next_row != NO_ROW) next_bias = lw;
+            } else {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int e = tile * A4_TILE + 16 * x;
+                    if (e < rq.rows) next_row[x] = pool_row(a.pool, b, h, e);
+                }
             }
         };
+        uint32_t gone = 0;                                       // two bits per stage: halves that are on no page
         auto fetch = [&](int stage, bool any) {
             if (any) {
-                bias[stage * A4_TILE + lane] = next_bias;
-                const uint32_t dst = ring_u32 + stage * C::TILE_BYTES;
+                const uint32_t dst = ring_u32 + stage * C::TILE_BYTES + lane * 16;
+                if constexpr (LIST) {
+                    bias[stage * A4_TILE + lane] = next_bias;
 #pragma unroll
-                for (int i = 0; i < R::CHUNKS; ++i) {
-                    const int c = i * 32 + lane, row = c / R::CHUNKS, chunk = c - row * R::CHUNKS;
-                    const uint32_t from = __shfl_sync(0xffffffffu, next_row, row);
-                    // (a row that is not there is filled with zeros: codes and scales of 0)
-                    cp16(dst + c * 16, a.pool.rows + (from != NO_ROW ? (uint64_t)from * R::BYTES + chunk * 16 : 0), from != NO_ROW);
+                    for (int i = 0; i < R::CHUNKS; ++i) {
+                        const int c = i * 32 + lane, row = c / R::CHUNKS, chunk = c - row * R::CHUNKS;
+                        const uint32_t from = __shfl_sync(0xffffffffu, next_row[0], row);
+                        // (a row that is not there is filled with zeros: codes and scales of 0)
+                        cp16(dst + i * 512, a.pool.rows + (from != NO_ROW ? (uint64_t)from * R::BYTES + chunk * 16 : 0), from != NO_ROW);
+                    }
+                } else {
+                    const bool there0 = next_row[0] != NO_ROW, there1 = next_row[1] != NO_ROW;
+                    gone = (gone & ~(3u << (2 * stage))) | ((there0 ? 0u : 1u) << (2 * stage)) | ((there1 ? 0u : 2u) << (2 * stage));
+                    const unsigned char *p0 = a.pool.rows + (there0 ? (uint64_t)next_row[0] * R::BYTES + lane * 16 : 0);
+                    // (the second half begins with chunk 16 CHUNKS, in the middle of the middle round)
+                    const unsigned char *p1 = a.pool.rows + (there1 ? (uint64_t)next_row[1] * R::BYTES + lane * 16 : 0);
+                    constexpr int MID = R::CHUNKS / 2;
+#pragma unroll
+                    for (int i = 0; i < MID; ++i) cp16(dst + i * 512, p0 + (there0 ? i * 512 : 0), there0);
+                    const bool up = lane >= 16;
+                    cp16(dst + MID * 512, up ? p1 - (there1 ? 256 : 0) : p0 + (there0 ? MID * 512 : 0), up ? there1 : there0);
+#pragma unroll
+                    for (int i = MID + 1; i < R::CHUNKS; ++i) cp16(dst + i * 512, p1 + (there1 ? i * 512 - MID * 512 - 256 : 0), there1);
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
@@ -322,6 +344,7 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
             __syncwarp();
             const unsigned char *rows = ring + stage * C::TILE_BYTES;
             const float *rb = bias + stage * A4_TILE;
+            const uint32_t gone_of = (gone >> (2 * stage)) & 3u;
             {
                 // the stage read in the last round is free
                 const int to = stage + A4_STAGES - 1;
@@ -335,7 +358,10 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
             // a value that is NaN must not reach a vector that does not see its row through 0 x NaN: such scales are taken out here and put
             // back as NaN sums of those that see it
             uint32_t nan_groups = 0, nan_rows = 0;
-            if (cut) {
+            const uint32_t gone_now = LIST ? 0u : gone_of;
+            if (!LIST && cut) {
+                // rows behind the last one came with their page, whatever they hold: nothing
+                if (tile * A4_TILE + lane >= rq.rows) *reinterpret_cast<uint4 *>(ring + (rows - ring) + lane * R::BYTES + R::SCALES) = make_uint4(0u, 0u, 0u, 0u);
                 unsigned char *vscale = ring + (rows - ring) + lane * R::BYTES + R::SCALES + R::GROUPS;
 #pragma unroll
                 for (int i = 0; i < R::GROUPS; ++i)
@@ -406,22 +432,41 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
             float top[NT][2];
 #pragma unroll
             for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY;
+            if (!LIST && (cut || gone_now)) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int at = tile * A4_TILE + kb * 16 + x * 8 + g;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                const bool out = at >= seen[n][y] || ((gone_now >> kb) & 1u);
+                                s[kb][n][2 * x + y] = out ? -INFINITY : s[kb][n][2 * x + y] * qs[n][y];
+                            }
+                    }
+            } else {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const float lw = LIST ? rb[kb * 16 + x * 8 + g] : 0.f;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                float &z = s[kb][n][2 * x + y];
+                                z = LIST ? fmaf(z, qs[n][y], lw) : z * qs[n][y];
+                            }
+                    }
+            }
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int at = kb * 16 + x * 8 + g;
-                    const float lw = rb[at];
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            float &z = s[kb][n][2 * x + y];
-                            z = fmaf(z, qs[n][y], lw);
-                            if (lw == -INFINITY || (cut && tile * A4_TILE + at >= seen[n][y])) z = -INFINITY;
-                            top[n][y] = fmaxf(top[n][y], z);
-                        }
-                }
+                    for (int y = 0; y < 2; ++y) top[n][y] = fmaxf(top[n][y], fmaxf(s[kb][n][y], s[kb][n][2 + y]));
             bool moved = false;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -589,13 +634,11 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                     for (int e = 0; e < EACH; ++e) store_from(to, sub + e * PER, acc[e] * inv);
                 }
             } else {
-                float *to = a.part + ((int64_t)(2 * blockIdx.x + (first_segment ? 0 : 1)) * N + v) * (D + 2);
+                const int64_t slot = (2 * blockIdx.x + (first_segment ? 0 : 1)) * N + v;
+                float *to = a.part + slot * D;
 #pragma unroll
                 for (int e = 0; e < EACH; ++e) to[sub + e * PER] = acc[e];
-                if (sub == 0) {
-                    to[D] = m;
-                    to[D + 1] = den;
-                }
+                if (sub == 0) reinterpret_cast<float2 *>(a.part + (int64_t)2 * gridDim.x * N * D)[slot] = make_float2(m, den);
             }
         }
         __syncthreads();
@@ -603,12 +646,16 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
 }
 
 // A CTA per problem (request, KV head, group): joins the parts of the stretches that share it, in their order.
+constexpr int A4_MERGE_THREADS = 256;
+constexpr int A4_MERGE_PARTS = 32;       // parts whose shares are held at a time
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(A4_THREADS) attend4_merge_kernel(const __grid_constant__ Attend4Args a, int ctas_launched, int max_groups)
+__global__ void __launch_bounds__(A4_MERGE_THREADS) attend4_merge_kernel(const __grid_constant__ Attend4Args a, int ctas_launched, int max_groups)
 {
-    constexpr int N = 8 * NT;
-    constexpr int PER = A4_THREADS / N, EACH = D / PER;
-    __shared__ int64_t prefix[A4_MAX_BATCH + 1], part[A4_WARPS];
+    constexpr int N = 8 * NT, EACH = N * D / A4_MERGE_THREADS, ROWS = A4_MERGE_THREADS / N;
+    extern __shared__ __align__(16) unsigned char smem[];
+    int64_t *prefix = reinterpret_cast<int64_t *>(smem);
+    __shared__ int64_t part[A4_MERGE_THREADS / 32];
+    __shared__ float top[ROWS][N], share[A4_MERGE_PARTS][N], den_of[A4_MERGE_PARTS][N];
     cudaGridDependencySynchronize();
     const int64_t total = lay_line(a, N, prefix, part);
     const int ctas = stretches(total, ctas_launched);
@@ -616,67 +663,81 @@ __global__ void __launch_bounds__(A4_THREADS) attend4_merge_kernel(const __grid_
     const int h = rest / max_groups, group = rest % max_groups;
     const Request rq = request_at(a, b, N);
     if (group >= rq.groups) return;
-    const int64_t f0 = prefix[b] + (int64_t)(h * rq.groups + group) * rq.tiles, f1 = f0 + rq.tiles;
+    const int64_t f0 = prefix[b] + (int64_t)(h * rq.groups + group) * rq.places, f1 = f0 + rq.places;
     // stretch c is [total c / ctas, total (c + 1) / ctas): the one that place f is in
-    const int64_t c0 = ((f0 + 1) * ctas - 1) / total, c1 = (f1 * ctas - 1) / total;
+    const int64_t c0 = ((f0 + A4_START + 1) * ctas - 1) / total, c1 = (f1 * ctas - 1) / total;
     if (c0 == c1) return;
-    const int v = threadIdx.x / PER, sub = threadIdx.x % PER;
-    auto slot = [&](int64_t c) {
-        const bool first = c > c0 || total * c / ctas == f0;     // the stretch begins with this problem
-        return a.part + ((2 * c + (first ? 0 : 1)) * N + v) * (D + 2);
-    };
+    const int count = (int)(c1 - c0 + 1);
+    // its second segment at most: the first stretch may have begun with another problem
+    const int64_t slot0 = 2 * c0 + (total * c0 / ctas >= f0 ? 0 : 1);
+    auto slot = [&](int i) { return i == 0 ? slot0 : 2 * (c0 + i); };
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part + (int64_t)2 * ctas_launched * N * D);
+    const int v = threadIdx.x % N, r = threadIdx.x / N;
     float m = -INFINITY;
-    for (int64_t c = c0; c <= c1; ++c) m = fmaxf(m, slot(c)[D]);
-    float den = 0.f, acc[EACH];
+    for (int i = r; i < count; i += ROWS) m = fmaxf(m, ml[slot(i) * N + v].x);
+    top[r][v] = m;
+    __syncthreads();
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) acc[e] = 0.f;
-    for (int64_t c = c0; c <= c1; ++c) {
-        const float *from = slot(c);
-        if (from[D] == -INFINITY) continue;
-        const float share = exp2_fast(from[D] - m);
-        den = fmaf(from[D + 1], share, den);
+    for (int i = 0; i < ROWS; ++i) m = fmaxf(m, top[i][v]);
+    float den[EACH], acc[EACH];
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) acc[e] = fmaf(from[sub + e * PER], share, acc[e]);
+    for (int e = 0; e < EACH; ++e) den[e] = acc[e] = 0.f;
+    for (int i0 = 0; i0 < count; i0 += A4_MERGE_PARTS) {
+        const int here = min(A4_MERGE_PARTS, count - i0);
+        for (int i = r; i < here; i += ROWS) {
+            const float2 x = ml[slot(i0 + i) * N + v];
+            share[i][v] = x.x == -INFINITY ? 0.f : exp2_fast(x.x - m);
+            den_of[i][v] = x.y;
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int i = 0; i < here; ++i) {
+            const float *from = a.part + slot(i0 + i) * N * D + threadIdx.x;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const int ve = (threadIdx.x + e * A4_MERGE_THREADS) / D;
+                acc[e] = fmaf(from[e * A4_MERGE_THREADS], share[i][ve], acc[e]);
+                den[e] = fmaf(den_of[i][ve], share[i][ve], den[e]);
+            }
+        }
+        __syncthreads();
     }
     const int vec0 = group * N;
-    if (v >= rq.tokens * a.rep - vec0) return;
-    const int vv = vec0 + v, tok = vv / a.rep, head = h * a.rep + vv % a.rep;
-    T *to = (T *)a.o + (a.cu ? (int64_t)(rq.first_token + tok) * a.os[2] : b * a.os[0] + tok * a.os[2]) + head * a.os[1];
-    const float inv = m == -INFINITY ? 0.f : 1.f / den;
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) store_from(to, sub + e * PER, acc[e] * inv);
+    for (int e = 0; e < EACH; ++e) {
+        const int x = threadIdx.x + e * A4_MERGE_THREADS, vv = vec0 + x / D;
+        if (vv >= rq.tokens * a.rep) continue;
+        const int tok = vv / a.rep, head = h * a.rep + vv % a.rep;
+        T *to = (T *)a.o + (a.cu ? (int64_t)(rq.first_token + tok) * a.os[2] : b * a.os[0] + tok * a.os[2]) + head * a.os[1];
+        store_from(to, x % D, den[e] == 0.f ? 0.f : acc[e] / den[e]);
+    }
 }
 
-template <typename T, int D, int NT, int PARTS> int attend4_ctas(int *out)
-{
-    using C = A4<D, NT, PARTS>;
-    auto kern = attend4_kernel<T, D, NT, PARTS>;
-    ELM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::TOTAL));
-    int per_sm = 0;
-    ELM_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, A4_THREADS, C::TOTAL));
-    *out = (per_sm < 1 ? 1 : per_sm) * device_sm_count();
-    return ELM_OK;
-}
 constexpr int A4_MAX_CTAS_PER_SM = 8;    // what the workspace has room for
 
-template <typename T, int D, int NT, int PARTS> int launch_attend4(const Attend4Args &a, cudaStream_t st)
+template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_form(const Attend4Args &a, cudaStream_t st)
 {
     using C = A4<D, NT, PARTS>;
-    int ctas = 0;
-    const int rc = attend4_ctas<T, D, NT, PARTS>(&ctas);
-    if (rc != ELM_OK) return rc;
-    const int most = A4_MAX_CTAS_PER_SM * device_sm_count();
-    if (ctas > most) ctas = most;
+    auto kern = attend4_kernel<T, D, NT, PARTS, LIST>;
+    const int smem = C::total(a.batch);
+    ELM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    int per_sm = 0;
+    ELM_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, A4_THREADS, smem));
+    per_sm = per_sm < 1 ? 1 : (per_sm > A4_MAX_CTAS_PER_SM ? A4_MAX_CTAS_PER_SM : per_sm);
     const int max_groups = (int)(((int64_t)a.n_q * a.rep + C::N - 1) / C::N);
     const int64_t problems = (int64_t)a.batch * a.pool.kv_heads * max_groups;
     if (problems > 0x7fffffff) return ELM_ERR_SHAPE;
     // no more CTAs than the longest line of tiles has stretches
-    const int64_t places = problems * ((a.n_kv + A4_TILE - 1) / A4_TILE);
-    const int grid = stretches(places, ctas);
-    ELM_CUDA_TRY(launch_after(attend4_kernel<T, D, NT, PARTS>, dim3((unsigned)grid), dim3(A4_THREADS), C::TOTAL, st, a));
-    ELM_CUDA_TRY(launch_after(attend4_merge_kernel<T, D, NT>, dim3((unsigned)problems), dim3(A4_THREADS), 0, st, a, grid, max_groups));
+    const int64_t places = problems * (A4_START + (a.n_kv + A4_TILE - 1) / A4_TILE);
+    const int grid = stretches(places, per_sm * device_sm_count());
+    ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)grid), dim3(A4_THREADS), smem, st, a));
+    ELM_CUDA_TRY(launch_after(attend4_merge_kernel<T, D, NT>, dim3((unsigned)problems), dim3(A4_MERGE_THREADS), (a.batch + 1) * 8, st, a, grid, max_groups));
     count_launches(2);
     return cuda_status(cudaGetLastError());
+}
+template <typename T, int D, int NT, int PARTS> int launch_attend4(const Attend4Args &a, cudaStream_t st)
+{
+    return a.idx ? launch_attend4_form<T, D, NT, PARTS, true>(a, st) : launch_attend4_form<T, D, NT, PARTS, false>(a, st);
 }
 
 bool zeros(const int64_t (&s)[3]) { return s[0] == 0 && s[1] == 0 && s[2] == 0; }
