@@ -436,22 +436,13 @@ def attend_static_status(Q, K, n_core: int, precision="fp32") -> int:
 # ------------------------------------------------------------------------------------------------
 # rotary positions, pages, rows held in 4 bits
 # ------------------------------------------------------------------------------------------------
-class _OnDevice:
-    """The calls below run on their tensors' device, on its current stream, whatever the current device is."""
+class _On:
+    """The calls below run on their tensors' device, on its current stream, whatever the current device is: ``with _On(device)``."""
 
-    def __init__(self, *tensors):
-        first = tensors[0]
-        for t in tensors:
-            if t is None:
-                continue
-            if not t.is_cuda:
-                if not torch.cuda.is_available():
-                    raise ElmError("no CUDA device: the library has no CPU fallback")
-                raise ElmError("tensors must be CUDA tensors")
-            if t.device != first.device:
-                raise ElmError("tensors must be on one device")
-        self.index = first.device.index
-        self.other = None
+    __slots__ = ("index", "other")
+
+    def __init__(self, index):
+        self.index, self.other = index, None
 
     def __enter__(self):
         if torch.cuda.current_device() != self.index:
@@ -461,6 +452,27 @@ class _OnDevice:
     def __exit__(self, *exc):
         if self.other is not None:
             self.other.__exit__(*exc)
+
+
+def _device(first, *tensors):
+    """Ordinal of the one device that the tensors (or None) are on."""
+    index = first.get_device()
+    if index < 0:
+        _require_cuda(first)
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ElmError("tensors must be CUDA tensors of one device")
+    return index
+
+
+class _Kept(dict):
+    """What a call has found out about sizes, strides and types (nothing of the tensors themselves), for the next one with the same."""
+
+    def keep(self, key, value):
+        if len(self) >= 256:
+            self.clear()
+        self[key] = value
+        return value
 
 
 def _rows(x, dims, what):
@@ -514,6 +526,7 @@ class Rope:
                                                    ctypes.byref(scale)), "elm_rope_frequencies")
         self.scale = scale.value
         self._freq_ptr = ctypes.cast(self._freq, ctypes.POINTER(ctypes.c_double))
+        self._kept = _Kept()
 
     @property
     def inv_freq(self):
@@ -523,27 +536,46 @@ class Rope:
 def rope(X, positions, rope: Rope, inverse=False, out=None):
     """elm_rope: X [B, H, n, d] (any strides, a head's numbers side by side) rotated by positions, an int32 tensor [B, n] or the first
     position of every sequence; ``inverse``: rotated back (the gradient).  ``out``: X itself, or another tensor of its shape."""
-    lib = load_library()
-    tensors = [X, out, positions if isinstance(positions, torch.Tensor) else None]
-    with _OnDevice(*tensors):
-        X, xs = _rows(X, 4, "X")
-        B, H, n, d = X.shape
-        O = out if out is not None else torch.empty(X.shape, dtype=X.dtype, device=X.device)
-        if O.shape != X.shape or O.dtype != X.dtype:
-            raise ElmError("out must have X's shape and dtype")
-        os_ = O.stride()
+    tensor = isinstance(positions, torch.Tensor)
+    with _On(_device(X, out, positions if tensor else None)):
+        key = (X.shape, X.stride(), X.dtype, inverse, positions.shape if tensor else None)
         if out is not None:
-            if (os_[-1] != 1 and d > 1) or not any(os_[:-1]) and O.numel() > d:
-                raise ElmError("out: the numbers of a head must lie side by side, rows apart")
-        p = RopeParams(B, H, n, d, _storage_code(X), rope.rotary_dim, rope.layout, int(bool(inverse)), rope.scale, rope._freq_ptr)
-        p.x_stride[:] = xs[:3]
-        p.out_stride[:] = os_[:3]
-        if isinstance(positions, torch.Tensor):
-            pos, first = _int32(positions, "positions", (B, n)).data_ptr(), 0
+            key += (out.shape, out.stride(), out.dtype)
+        p = rope._kept.get(key)
+        if p is None:
+            Y, xs = _rows(X, 4, "X")
+            if Y is not X:                                      # (a broadcast of one row)
+                return _rope_of_copy(X, Y, positions, rope, inverse, out)
+            B, H, n, d = X.shape
+            if out is not None:
+                if out.shape != X.shape or out.dtype != X.dtype:
+                    raise ElmError("out must have X's shape and dtype")
+                os_ = out.stride()
+                if (os_[-1] != 1 and d > 1) or not any(os_[:-1]) and out.numel() > d:
+                    raise ElmError("out: the numbers of a head must lie side by side, rows apart")
+            if tensor:
+                _int32(positions, "positions", (B, n))
+            p = RopeParams(B, H, n, d, _storage_code(X), rope.rotary_dim, rope.layout, int(bool(inverse)), rope.scale, rope._freq_ptr)
+            p.x_stride[:] = xs[:3]
+            p.out_stride[:] = os_[:3] if out is not None else (0, 0, 0)
+            rope._kept.keep(key, p)
+        if tensor:
+            if positions.dtype is not torch.int32 or not positions.is_contiguous():
+                raise ElmError("positions must be a contiguous int32 tensor")
+            pos, first = positions.data_ptr(), 0
         else:
             pos, first = None, int(positions)
-        _check(lib.elm_rope(X.data_ptr(), pos, first, ctypes.byref(p), O.data_ptr(), _stream()), "elm_rope")
+        O = out if out is not None else torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        rc = load_library().elm_rope(X.data_ptr(), pos, first, p, O.data_ptr(), _stream())
+    if rc:
+        _check(rc, "elm_rope")
     return O
+
+
+def _rope_of_copy(X, Y, positions, rope_, inverse, out):
+    if out is X:
+        raise ElmError("out: rows must lie apart")
+    return rope(Y, positions, rope_, inverse, out)
 
 
 class PagePlan:
@@ -552,41 +584,48 @@ class PagePlan:
     __slots__ = ("start", "length", "free_count", "cu", "positions", "slots")
 
 
+_plan_kept = _Kept()
+
+
 def page_plan(table, length, n_new, free, free_count, page_rows: int, max_tokens: int, length_out=None, free_count_out=None) -> PagePlan:
     """elm_page_plan: pages, positions and slots of the n_new [B] tokens that come to requests of length [B].  ``table`` [B, max_pages]
     gets the new pages' numbers; length_out and free_count_out may be length and free_count."""
-    lib = load_library()
-    with _OnDevice(table, length, n_new, free, free_count, length_out, free_count_out):
-        B, max_pages = _int32(table, "table").shape
-        _int32(length, "length", (B,)), _int32(n_new, "n_new", (B,)), _int32(free, "free"), _int32(free_count, "free_count", (1,))
-        # (one allocation for all that comes out; every part on a 16-byte boundary)
-        up = lambda n: -(-n // 4) * 4  # noqa: E731
-        need = 2 * up(B) + 4 + up(B + 1) + 2 * up(max_tokens)
-        buf = torch.empty(need, dtype=torch.int32, device=table.device)
-        at = 0
-
-        def part(n):
-            nonlocal at
-            t = buf[at:at + n]
-            at += up(n)
-            return t
+    with _On(_device(table, length, n_new, free, free_count, length_out, free_count_out)):
+        key = (table.shape, length.shape, n_new.shape, free.shape, free_count.shape, page_rows, max_tokens)
+        kept = _plan_kept.get(key)
+        if kept is None:
+            if table.dim() != 2:
+                raise ElmError("table must be [B, max_pages]")
+            B, max_pages = table.shape
+            _int32(length, "length", (B,)), _int32(n_new, "n_new", (B,)), _int32(free, "free"), _int32(free_count, "free_count", (1,))
+            # one allocation for all that comes out; every part on a 16-byte boundary
+            sizes = [B, B, 1, B + 1, max(0, max_tokens), max(0, max_tokens)]
+            padded = [-(-n // 4) * 4 for n in sizes]
+            cuts = [x for n, m in zip(sizes, padded) for x in (n, m - n)]
+            kept = _plan_kept.keep(key, (PageParams(B, max_pages, page_rows, max_tokens, free.numel()), sum(padded), cuts))
+        p, total, cuts = kept
+        for t in (table, length, n_new, free, free_count):
+            if t.dtype is not torch.int32 or not t.is_contiguous():
+                raise ElmError("table, length, n_new, free and free_count must be contiguous int32 tensors")
+        buf = torch.empty(total, dtype=torch.int32, device=table.device)
         r = PagePlan()
-        r.start, r.length, r.free_count, r.cu, r.positions, r.slots = part(B), part(B), part(1), part(B + 1), part(max_tokens), part(max_tokens)
+        r.start, _, r.length, _, r.free_count, _, r.cu, _, r.positions, _, r.slots, _ = buf.split_with_sizes(cuts)
         if length_out is not None:
-            r.length = _int32(length_out, "length_out", (B,))
+            r.length = _int32(length_out, "length_out", length.shape)
         if free_count_out is not None:
             r.free_count = _int32(free_count_out, "free_count_out", (1,))
-        p = PageParams(B, max_pages, page_rows, max_tokens, free.numel())
-        _check(lib.elm_page_plan(table.data_ptr(), length.data_ptr(), n_new.data_ptr(), free.data_ptr(), free_count.data_ptr(),
-                                 ctypes.byref(p), r.start.data_ptr(), r.length.data_ptr(), r.free_count.data_ptr(), r.cu.data_ptr(),
-                                 r.positions.data_ptr(), r.slots.data_ptr(), _stream()), "elm_page_plan")
+        rc = load_library().elm_page_plan(table.data_ptr(), length.data_ptr(), n_new.data_ptr(), free.data_ptr(), free_count.data_ptr(), p,
+                                          r.start.data_ptr(), r.length.data_ptr(), r.free_count.data_ptr(), r.cu.data_ptr(),
+                                          r.positions.data_ptr(), r.slots.data_ptr(), _stream())
+    if rc:
+        _check(rc, "elm_page_plan")
     return r
 
 
 def page_release(table, length, done, free, free_count, page_rows: int):
     """elm_page_release: the pages of the requests with done [B] != 0 go back to the end of free; everything in place."""
     lib = load_library()
-    with _OnDevice(table, length, done, free, free_count):
+    with _On(_device(table, length, done, free, free_count)):
         B, max_pages = _int32(table, "table").shape
         _int32(length, "length", (B,)), _int32(done, "done", (B,)), _int32(free, "free"), _int32(free_count, "free_count", (1,))
         p = PageParams(B, max_pages, page_rows, 0, free.numel())
@@ -614,43 +653,67 @@ def _pool_d(rows):
     return d
 
 
+_append_kept = _Kept()
+
+
 def cache4_append(rows, K, V, slots, rope: Rope = None, positions=None, Q=None, q_out=None):
     """elm_cache4_append: K, V [T, Hkv, d] into the pool's rows slots [T] (a slot outside the pool: passed over), keys rotated by
     ``rope`` at positions [T].  Q [T, Hq, d] comes back rotated (in q_out, which may be Q; of tokens passed over, as q_out was)."""
-    lib = load_library()
-    with _OnDevice(rows, K, V, slots, positions, Q, q_out):
-        d = _pool_d(rows)
-        K, ks = _rows(K, 3, "K")
-        V, vs = _rows(V, 3, "V")
-        T, H = K.shape[:2]
-        if K.shape != V.shape or K.dtype != V.dtype or K.shape[2] != d or H != rows.shape[1]:
-            raise ElmError("K and V must be [tokens, kv_heads, d] of the pool's heads, of one dtype")
-        _int32(slots, "slots", (T,))
-        if rope is not None:
-            if positions is None:
-                raise ElmError("a rotation needs positions")
-            _int32(positions, "positions", (T,))
-        p = AppendParams(T, 0, H, d, _storage_code(K), rows.shape[2], rows.shape[0])
-        if rope is not None:
-            p.rotary_dim, p.layout, p.scale, p.inv_freq = rope.rotary_dim, rope.layout, rope.scale, rope._freq_ptr
-        p.k_stride[:] = ks[:2]
-        p.v_stride[:] = vs[:2]
-        O = None
+    with _On(_device(rows, K, V, slots, positions, Q, q_out)):
+        kept = _append_kept if rope is None else rope._kept
+        key = (rows.shape, K.shape, K.stride(), K.dtype, V.shape, V.stride(), V.dtype, slots.shape)
+        if positions is not None:
+            key += (positions.shape,)
         if Q is not None:
-            given = Q
-            Q, qs = _rows(Q, 3, "Q")
-            if Q.shape[0] != T or Q.shape[2] != d or Q.dtype != K.dtype:
-                raise ElmError("Q must be [tokens, q_heads, d] of K's dtype")
-            O = q_out if q_out is not None else torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
-            if O.shape != Q.shape or O.dtype != Q.dtype or O.stride(2) != 1 or (O is given and Q is not given):
-                raise ElmError("q_out must have Q's shape and dtype, the numbers of a head side by side")
-            if not any(O.stride()[:2]) and O.numel() > d:
-                raise ElmError("q_out: rows must lie apart")
-            p.q_heads = Q.shape[1]
-            p.q_stride[:] = qs[:2]
-            p.q_out_stride[:] = O.stride()[:2]
-        _check(lib.elm_cache4_append(_ptr(Q), K.data_ptr(), V.data_ptr(), _ptr(positions) if rope is not None else None, slots.data_ptr(),
-                                     ctypes.byref(p), _ptr(O), rows.data_ptr(), _stream()), "elm_cache4_append")
+            key += (Q.shape, Q.stride(), Q.dtype)
+            if q_out is not None:
+                key += (q_out.shape, q_out.stride(), q_out.dtype)
+        p = kept.get(key)
+        if p is None:
+            d = _pool_d(rows)
+            K2, ks = _rows(K, 3, "K")
+            V2, vs = _rows(V, 3, "V")
+            Q2, qs = (None, None) if Q is None else _rows(Q, 3, "Q")
+            if K2 is not K or V2 is not V or Q2 is not Q:       # (a broadcast of one row)
+                if Q2 is not Q and q_out is Q:
+                    raise ElmError("q_out: rows must lie apart")
+                return cache4_append(rows, K2, V2, slots, rope, positions, Q2, q_out)
+            T, H = K.shape[:2]
+            if K.shape != V.shape or K.dtype != V.dtype or K.shape[2] != d or H != rows.shape[1]:
+                raise ElmError("K and V must be [tokens, kv_heads, d] of the pool's heads, of one dtype")
+            _int32(slots, "slots", (T,))
+            if rope is not None:
+                if positions is None:
+                    raise ElmError("a rotation needs positions")
+                _int32(positions, "positions", (T,))
+            p = AppendParams(T, 0, H, d, _storage_code(K), rows.shape[2], rows.shape[0])
+            if rope is not None:
+                p.rotary_dim, p.layout, p.scale, p.inv_freq = rope.rotary_dim, rope.layout, rope.scale, rope._freq_ptr
+            p.k_stride[:] = ks[:2]
+            p.v_stride[:] = vs[:2]
+            if Q is not None:
+                if Q.shape[0] != T or Q.shape[2] != d or Q.dtype != K.dtype:
+                    raise ElmError("Q must be [tokens, q_heads, d] of K's dtype")
+                p.q_heads = Q.shape[1]
+                p.q_stride[:] = qs[:2]
+                if q_out is not None:
+                    if q_out.shape != Q.shape or q_out.dtype != Q.dtype or q_out.stride(2) != 1:
+                        raise ElmError("q_out must have Q's shape and dtype, the numbers of a head side by side")
+                    if not any(q_out.stride()[:2]) and q_out.numel() > d:
+                        raise ElmError("q_out: rows must lie apart")
+                    p.q_out_stride[:] = q_out.stride()[:2]
+            kept.keep(key, p)
+        if rows.dtype is not torch.uint8 or not rows.is_contiguous() or slots.dtype is not torch.int32 or not slots.is_contiguous():
+            raise ElmError("rows must be contiguous uint8 and slots contiguous int32")
+        pos = None
+        if rope is not None:
+            if positions.dtype is not torch.int32 or not positions.is_contiguous():
+                raise ElmError("positions must be contiguous int32")
+            pos = positions.data_ptr()
+        O = None if Q is None else q_out if q_out is not None else torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        rc = load_library().elm_cache4_append(_ptr(Q), K.data_ptr(), V.data_ptr(), pos, slots.data_ptr(), p, _ptr(O), rows.data_ptr(), _stream())
+    if rc:
+        _check(rc, "elm_cache4_append")
     return O
 
 
@@ -660,32 +723,54 @@ def _cache4_params(rows, table, q_heads, dtype_code, n_kv, n_q=1, n_tokens=0, ca
     return Cache4Params(B, q_heads, rows.shape[1], d, dtype_code, rows.shape[2], rows.shape[0], max_pages, n_kv, n_q, n_tokens, int(bool(causal)))
 
 
+_cache4_kept = _Kept()
+
+
 def cache4_read(rows, table, n: int, idx=None, length=None, dtype=torch.bfloat16, out=None):
     """elm_cache4_read -> K, V [B, Hkv, n, d]: rows 0 .. n - 1 of every request, or rows idx [B, Hkv, n]; a row that is not there (past
     length [B], on no page) is zeros.  ``out``: a pair of tensors for them."""
-    lib = load_library()
-    with _OnDevice(rows, table, idx, length, *(out or ())):
-        code = {torch.float32: ELM_F32, torch.bfloat16: ELM_BF16}.get(dtype)
-        if code is None:
-            raise ElmError(f"unsupported dtype {dtype}")
-        p = _cache4_params(rows, table, rows.shape[1], code, n)
-        shape = (p.batch, p.kv_heads, n, p.d)
-        if idx is not None:
-            _int32(idx, "idx", shape[:3])
-        if length is not None:
-            _int32(length, "length", shape[:1])
-        K, V = out if out is not None else (torch.empty(shape, dtype=dtype, device=rows.device), torch.empty(shape, dtype=dtype, device=rows.device))
-        if out is not None and any(tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() for t in out):
-            raise ElmError(f"out must be two contiguous tensors of shape {shape} and dtype {dtype}")
-        _check(lib.elm_cache4_read(rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(idx), ctypes.byref(p), K.data_ptr(), V.data_ptr(),
-                                   _stream()), "elm_cache4_read")
+    with _On(_device(rows, table, idx, length, *(out or ()))):
+        key = (rows.shape, table.shape, n, idx if idx is None else idx.shape, length if length is None else length.shape, dtype)
+        kept = _cache4_kept.get(key)
+        if kept is None:
+            code = {torch.float32: ELM_F32, torch.bfloat16: ELM_BF16}.get(dtype)
+            if code is None:
+                raise ElmError(f"unsupported dtype {dtype}")
+            p = _cache4_params(rows, table, rows.shape[1], code, n)
+            shape = (p.batch, p.kv_heads, n, p.d)
+            if idx is not None:
+                _int32(idx, "idx", shape[:3])
+            if length is not None:
+                _int32(length, "length", shape[:1])
+            kept = _cache4_kept.keep(key, (p, shape))
+        p, shape = kept
+        _int32_all(rows, table, idx, length)
+        if out is not None:
+            K, V = out
+            if any(tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() for t in out):
+                raise ElmError(f"out must be two contiguous tensors of shape {shape} and dtype {dtype}")
+        else:
+            K, V = torch.empty(shape, dtype=dtype, device=rows.device), torch.empty(shape, dtype=dtype, device=rows.device)
+        rc = load_library().elm_cache4_read(rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(idx), p, K.data_ptr(), V.data_ptr(), _stream())
+    if rc:
+        _check(rc, "elm_cache4_read")
     return K, V
+
+
+def _int32_all(rows, *tensors):
+    if rows.dtype is not torch.uint8 or not rows.is_contiguous():
+        raise ElmError("rows must be a contiguous uint8 tensor")
+    for t in tensors:
+        if t is not None and (t.dtype is not torch.int32 or not t.is_contiguous()):
+            raise ElmError("table, length, cu and idx must be contiguous int32 tensors")
 
 
 def _attend4_params(Q, rows, table, cu, idx, w, length, n_kv, max_q, causal, out):
     if (idx is None) == (length is None):
         raise ElmError("give either length (a request's rows) or idx and w (a list of them)")
-    Q, qs = _rows(Q, 3 if cu is not None else 4, "Q")
+    Q2, qs = _rows(Q, 3 if cu is not None else 4, "Q")
+    if Q2 is not Q:
+        return None                                             # (a broadcast of one row)
     if cu is not None:
         if max_q is None:
             raise ElmError("cu needs max_q, the most tokens of any request")
@@ -710,18 +795,18 @@ def _attend4_params(Q, rows, table, cu, idx, w, length, n_kv, max_q, causal, out
     else:
         _int32(length, "length", (p.batch,))
         p.n_kv = int(n_kv) if n_kv is not None else 0
-    O = out if out is not None else torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
-    if O.shape != Q.shape or O.dtype != Q.dtype or (O.stride(-1) != 1) or (not any(O.stride()[:-1]) and O.numel() > d):
-        raise ElmError("out must have Q's shape and dtype, the numbers of a head side by side")
-    os_ = O.stride()
     # dense tensors are told to the library as such: its tensor-core form takes no others
-    if cu is not None or not Q.is_contiguous():
+    if not Q.is_contiguous() or cu is not None:
         p.q_stride[:] = qs
-    if cu is not None:
-        p.o_stride[:] = (0, os_[1], os_[0])
-    elif not O.is_contiguous():
-        p.o_stride[:] = os_[:3]
-    return Q, O, p
+    if out is not None:
+        os_ = out.stride()
+        if out.shape != Q.shape or out.dtype != Q.dtype or os_[-1] != 1 or (not any(os_[:-1]) and out.numel() > d):
+            raise ElmError("out must have Q's shape and dtype, the numbers of a head side by side")
+        if cu is not None:
+            p.o_stride[:] = (0, os_[1], os_[0])
+        elif not out.is_contiguous():
+            p.o_stride[:] = os_[:3]
+    return p
 
 
 def cache4_attend_workspace_bytes(params: Cache4Params, with_list: bool) -> int:
@@ -735,12 +820,28 @@ def cache4_attend(Q, rows, table, length=None, idx=None, w=None, cu=None, max_q=
     """elm_cache4_attend: Q [B, Hq, n, d] over the rows of the requests of table [B, max_pages]: the first length [B] of them (n_kv: a bound
     of the lengths that the host knows; causal: a request's queries are its last tokens), or the list idx with weights w
     [B, Hkv, n_core].  With cu [B + 1]: Q [T, Hq, d], request b has the tokens cu[b] .. cu[b + 1] - 1, max_q at most.  O like Q."""
-    lib = load_library()
-    with _OnDevice(rows, Q, table, length, idx, w, cu, workspace, out):
-        Q, O, p = _attend4_params(Q, rows, table, cu, idx, w, length, n_kv, max_q, causal, out)
-        ws = workspace if workspace is not None else _workspace(cache4_attend_workspace_bytes(p, idx is not None), Q.device)
-        _check(lib.elm_cache4_attend(Q.data_ptr(), rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(cu), _ptr(idx), _ptr(w),
-                                     ctypes.byref(p), O.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "elm_cache4_attend")
+    device = _device(rows, Q, table, length, idx, w, cu, workspace, out)
+    with _On(device):
+        key = (device, Q.shape, Q.stride(), Q.dtype, rows.shape, table.shape, max_q, n_kv, causal,
+               length if length is None else length.shape, cu if cu is None else cu.shape,
+               idx if idx is None else (idx.shape, w if w is None else (w.shape, w.dtype, w.is_contiguous())),
+               out if out is None else (out.shape, out.stride(), out.dtype))
+        kept = _cache4_kept.get(key)
+        if kept is None:
+            p = _attend4_params(Q, rows, table, cu, idx, w, length, n_kv, max_q, causal, out)
+            if p is None:
+                if out is Q:
+                    raise ElmError("out: rows must lie apart")
+                return cache4_attend(Q.contiguous(), rows, table, length, idx, w, cu, max_q, n_kv, causal, workspace, out)
+            kept = _cache4_kept.keep(key, (p, cache4_attend_workspace_bytes(p, idx is not None)))
+        p, need = kept
+        _int32_all(rows, table, length, idx, cu)
+        ws = workspace if workspace is not None else torch.empty(need, dtype=torch.uint8, device=Q.device)
+        O = out if out is not None else torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        rc = load_library().elm_cache4_attend(Q.data_ptr(), rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(cu), _ptr(idx), _ptr(w), p,
+                                              O.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+    if rc:
+        _check(rc, "elm_cache4_attend")
     return O
 
 

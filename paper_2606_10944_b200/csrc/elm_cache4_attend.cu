@@ -21,6 +21,8 @@
 // stretch is finished there; the parts of one that several CTAs share go to the workspace and are joined by a second launch.
 #include <math.h>
 
+#include <atomic>
+
 #include "elm_attend.cuh"
 #include "elm_cache4.cuh"
 
@@ -31,9 +33,9 @@ constexpr int A4_WARPS = 4;
 constexpr int A4_THREADS = 32 * A4_WARPS;
 constexpr int A4_TILE = 32;              // rows of a warp's tile
 constexpr int A4_STAGES = 2;
-constexpr int A4_START = 8;              // what a problem's beginning and end cost, in tiles
-constexpr int A4_MAX_BATCH = 1024;
-constexpr int A4_CTA_PLACES = A4_START / 2 + A4_WARPS;     // a CTA's stretch holds at least these
+constexpr int A4_START = 12;              // what a problem's beginning and end cost, in tiles
+constexpr int A4_MAX_BATCH = 1024, A4_FEW = 127;                // requests of a call; of one whose line is short
+constexpr int A4_CTA_PLACES = 8;     // a CTA's stretch holds at least these
 constexpr float A4_LIFT = 8.f;           // probabilities are 2^8 times their share of the reference's
 constexpr float A4_SLACK = 6.f;          // how far the maximum may pass the reference: fp16 ends at 2^16
 
@@ -190,6 +192,8 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
     const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
 
     cudaGridDependencySynchronize();
+    // (the launch that joins the parts may come in as CTAs end: it waits for all of this one before it reads them)
+    cudaTriggerProgrammaticLaunchCompletion();
     const int64_t total = lay_line(a, N, prefix, reinterpret_cast<int64_t *>(smem));
     const int ctas = stretches(total, gridDim.x);
     if ((int)blockIdx.x >= ctas) return;
@@ -645,18 +649,22 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
     }
 }
 
-// A CTA per problem (request, KV head, group): joins the parts of the stretches that share it, in their order.
+// Joins the parts of a problem (request, KV head, group) that stretches share, in their order; a CTA per problem and slice of its numbers.
+// With few problems of many parts a problem's numbers are cut into slices, so that more CTAs read (8 problems of 32768 rows, 74 parts each:
+// one CTA per problem took longer than the attention).  Each number's parts are dealt to SHARE threads.
 constexpr int A4_MERGE_THREADS = 256;
-constexpr int A4_MERGE_PARTS = 32;       // parts whose shares are held at a time
-template <typename T, int D, int NT>
+constexpr int A4_MERGE_PARTS = 64;       // parts whose shares are held at a time
+template <typename T, int D, int NT, int SLICES>
 __global__ void __launch_bounds__(A4_MERGE_THREADS) attend4_merge_kernel(const __grid_constant__ Attend4Args a, int ctas_launched, int max_groups)
 {
-    constexpr int N = 8 * NT, EACH = N * D / A4_MERGE_THREADS, ROWS = A4_MERGE_THREADS / N;
+    constexpr int N = 8 * NT, SLICE = N * D / SLICES;            // numbers of a CTA
+    constexpr int SHARE = SLICE < A4_MERGE_THREADS ? A4_MERGE_THREADS / SLICE : 1, EACH = SLICE * SHARE / A4_MERGE_THREADS;
+    constexpr int ROWS = A4_MERGE_THREADS / N;
     extern __shared__ __align__(16) unsigned char smem[];
     int64_t *prefix = reinterpret_cast<int64_t *>(smem);
     __shared__ int64_t part[A4_MERGE_THREADS / 32];
-    __shared__ float top[ROWS][N], share[A4_MERGE_PARTS][N], den_of[A4_MERGE_PARTS][N];
-    cudaGridDependencySynchronize();
+    __shared__ float top[ROWS][N], share[A4_MERGE_PARTS][N], den_of[A4_MERGE_PARTS][N], sums[SHARE][2][SHARE > 1 ? SLICE : 1];
+    // lengths and cu are older than the launch before this one, whose CTAs let this one start when they had waited for them
     const int64_t total = lay_line(a, N, prefix, part);
     const int ctas = stretches(total, ctas_launched);
     const int b = blockIdx.x / (a.pool.kv_heads * max_groups), rest = blockIdx.x % (a.pool.kv_heads * max_groups);
@@ -667,6 +675,7 @@ __global__ void __launch_bounds__(A4_MERGE_THREADS) attend4_merge_kernel(const _
     // stretch c is [total c / ctas, total (c + 1) / ctas): the one that place f is in
     const int64_t c0 = ((f0 + A4_START + 1) * ctas - 1) / total, c1 = (f1 * ctas - 1) / total;
     if (c0 == c1) return;
+    cudaGridDependencySynchronize();
     const int count = (int)(c1 - c0 + 1);
     // its second segment at most: the first stretch may have begun with another problem
     const int64_t slot0 = 2 * c0 + (total * c0 / ctas >= f0 ? 0 : 1);
@@ -679,6 +688,7 @@ __global__ void __launch_bounds__(A4_MERGE_THREADS) attend4_merge_kernel(const _
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) m = fmaxf(m, top[i][v]);
+    const int sub = SHARE > 1 ? threadIdx.x / SLICE : 0, x0 = blockIdx.y * SLICE + (SHARE > 1 ? threadIdx.x % SLICE : threadIdx.x);
     float den[EACH], acc[EACH];
 #pragma unroll
     for (int e = 0; e < EACH; ++e) den[e] = acc[e] = 0.f;
@@ -690,22 +700,33 @@ __global__ void __launch_bounds__(A4_MERGE_THREADS) attend4_merge_kernel(const _
             den_of[i][v] = x.y;
         }
         __syncthreads();
-#pragma unroll 4
-        for (int i = 0; i < here; ++i) {
-            const float *from = a.part + slot(i0 + i) * N * D + threadIdx.x;
+#pragma unroll 8
+        for (int i = sub; i < here; i += SHARE) {
+            const float *from = a.part + slot(i0 + i) * N * D + x0;
 #pragma unroll
             for (int e = 0; e < EACH; ++e) {
-                const int ve = (threadIdx.x + e * A4_MERGE_THREADS) / D;
+                const int ve = (x0 + e * A4_MERGE_THREADS) / D;
                 acc[e] = fmaf(from[e * A4_MERGE_THREADS], share[i][ve], acc[e]);
                 den[e] = fmaf(den_of[i][ve], share[i][ve], den[e]);
             }
         }
         __syncthreads();
     }
+    if constexpr (SHARE > 1) {
+        sums[sub][0][threadIdx.x % SLICE] = acc[0];
+        sums[sub][1][threadIdx.x % SLICE] = den[0];
+        __syncthreads();
+        if (sub) return;
+#pragma unroll
+        for (int i = 1; i < SHARE; ++i) {
+            acc[0] += sums[i][0][threadIdx.x];
+            den[0] += sums[i][1][threadIdx.x];
+        }
+    }
     const int vec0 = group * N;
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
-        const int x = threadIdx.x + e * A4_MERGE_THREADS, vv = vec0 + x / D;
+        const int x = x0 + e * A4_MERGE_THREADS, vv = vec0 + x / D;
         if (vv >= rq.tokens * a.rep) continue;
         const int tok = vv / a.rep, head = h * a.rep + vv % a.rep;
         T *to = (T *)a.o + (a.cu ? (int64_t)(rq.first_token + tok) * a.os[2] : b * a.os[0] + tok * a.os[2]) + head * a.os[1];
@@ -719,11 +740,19 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
 {
     using C = A4<D, NT, PARTS>;
     auto kern = attend4_kernel<T, D, NT, PARTS, LIST>;
-    const int smem = C::total(a.batch);
-    ELM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    int per_sm = 0;
-    ELM_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, A4_THREADS, smem));
-    per_sm = per_sm < 1 ? 1 : (per_sm > A4_MAX_CTAS_PER_SM ? A4_MAX_CTAS_PER_SM : per_sm);
+    // CTAs per SM, asked once per device and size of the line (threads that meet here first find the same answer)
+    static std::atomic<int> known[64][2];
+    const bool big = a.batch > A4_FEW;
+    const int smem = C::total(big ? A4_MAX_BATCH : A4_FEW);
+    int dev = 0;
+    ELM_CUDA_TRY(cudaGetDevice(&dev));
+    int per_sm = dev < 64 ? known[dev][big].load(std::memory_order_relaxed) : 0;
+    if (per_sm == 0) {
+        ELM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::total(A4_MAX_BATCH)));
+        ELM_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, A4_THREADS, smem));
+        per_sm = per_sm < 1 ? 1 : (per_sm > A4_MAX_CTAS_PER_SM ? A4_MAX_CTAS_PER_SM : per_sm);
+        if (dev < 64) known[dev][big].store(per_sm, std::memory_order_relaxed);
+    }
     const int max_groups = (int)(((int64_t)a.n_q * a.rep + C::N - 1) / C::N);
     const int64_t problems = (int64_t)a.batch * a.pool.kv_heads * max_groups;
     if (problems > 0x7fffffff) return ELM_ERR_SHAPE;
@@ -731,7 +760,10 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
     const int64_t places = problems * (A4_START + (a.n_kv + A4_TILE - 1) / A4_TILE);
     const int grid = stretches(places, per_sm * device_sm_count());
     ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)grid), dim3(A4_THREADS), smem, st, a));
-    ELM_CUDA_TRY(launch_after(attend4_merge_kernel<T, D, NT>, dim3((unsigned)problems), dim3(A4_MERGE_THREADS), (a.batch + 1) * 8, st, a, grid, max_groups));
+    constexpr int MANY = C::N * D / 128;                         // slices of 128 numbers where the problems alone are few
+    auto join = problems * MANY <= 2 * device_sm_count() ? attend4_merge_kernel<T, D, NT, MANY> : attend4_merge_kernel<T, D, NT, 1>;
+    const dim3 join_grid((unsigned)problems, problems * MANY <= 2 * device_sm_count() ? MANY : 1);
+    ELM_CUDA_TRY(launch_after(join, join_grid, dim3(A4_MERGE_THREADS), (a.batch + 1) * 8, st, a, grid, max_groups));
     count_launches(2);
     return cuda_status(cudaGetLastError());
 }
