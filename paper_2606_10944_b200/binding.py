@@ -565,7 +565,7 @@ def rope(X, positions, rope: Rope, inverse=False, out=None):
             pos, first = positions.data_ptr(), 0
         else:
             pos, first = None, int(positions)
-        O = out if out is not None else torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        O = out if out is not None else torch.empty_like(X, memory_format=torch.contiguous_format)
         rc = load_library().elm_rope(X.data_ptr(), pos, first, p, O.data_ptr(), _stream())
     if rc:
         _check(rc, "elm_rope")
@@ -598,18 +598,16 @@ def page_plan(table, length, n_new, free, free_count, page_rows: int, max_tokens
                 raise ElmError("table must be [B, max_pages]")
             B, max_pages = table.shape
             _int32(length, "length", (B,)), _int32(n_new, "n_new", (B,)), _int32(free, "free"), _int32(free_count, "free_count", (1,))
-            # one allocation for all that comes out; every part on a 16-byte boundary
-            sizes = [B, B, 1, B + 1, max(0, max_tokens), max(0, max_tokens)]
-            padded = [-(-n // 4) * 4 for n in sizes]
-            cuts = [x for n, m in zip(sizes, padded) for x in (n, m - n)]
-            kept = _plan_kept.keep(key, (PageParams(B, max_pages, page_rows, max_tokens, free.numel()), sum(padded), cuts))
+            # (one allocation for all that comes out)
+            sizes = [max(0, max_tokens), max(0, max_tokens), B, B, B + 1, 1]
+            kept = _plan_kept.keep(key, (PageParams(B, max_pages, page_rows, max_tokens, free.numel()), sum(sizes), sizes))
         p, total, cuts = kept
         for t in (table, length, n_new, free, free_count):
             if t.dtype is not torch.int32 or not t.is_contiguous():
                 raise ElmError("table, length, n_new, free and free_count must be contiguous int32 tensors")
         buf = torch.empty(total, dtype=torch.int32, device=table.device)
         r = PagePlan()
-        r.start, _, r.length, _, r.free_count, _, r.cu, _, r.positions, _, r.slots, _ = buf.split_with_sizes(cuts)
+        r.positions, r.slots, r.start, r.length, r.cu, r.free_count = buf.split_with_sizes(cuts)
         if length_out is not None:
             r.length = _int32(length_out, "length_out", length.shape)
         if free_count_out is not None:
@@ -710,7 +708,7 @@ def cache4_append(rows, K, V, slots, rope: Rope = None, positions=None, Q=None, 
             if positions.dtype is not torch.int32 or not positions.is_contiguous():
                 raise ElmError("positions must be contiguous int32")
             pos = positions.data_ptr()
-        O = None if Q is None else q_out if q_out is not None else torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        O = None if Q is None else q_out if q_out is not None else torch.empty_like(Q, memory_format=torch.contiguous_format)
         rc = load_library().elm_cache4_append(_ptr(Q), K.data_ptr(), V.data_ptr(), pos, slots.data_ptr(), p, _ptr(O), rows.data_ptr(), _stream())
     if rc:
         _check(rc, "elm_cache4_append")
@@ -837,7 +835,7 @@ def cache4_attend(Q, rows, table, length=None, idx=None, w=None, cu=None, max_q=
         p, need = kept
         _int32_all(rows, table, length, idx, cu)
         ws = workspace if workspace is not None else torch.empty(need, dtype=torch.uint8, device=Q.device)
-        O = out if out is not None else torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        O = out if out is not None else torch.empty_like(Q, memory_format=torch.contiguous_format)
         rc = load_library().elm_cache4_attend(Q.data_ptr(), rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(cu), _ptr(idx), _ptr(w), p,
                                               O.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
     if rc:

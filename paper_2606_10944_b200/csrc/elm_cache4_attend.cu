@@ -19,6 +19,7 @@
 // What bounds it: reading each row once (144 bytes at d = 128).  The rows of all problems form one line of tiles, and every CTA takes an equal
 // stretch of it, whatever the requests' lengths are - they are on the device, and the stretch is found there.  A problem that lies in one
 // stretch is finished there; the parts of one that several CTAs share go to the workspace and are joined by a second launch.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include <atomic>
@@ -48,6 +49,8 @@ struct Attend4Args {
     float *part;                         // sums [2 * ctas][N][D], then (reference, denominator) [2 * ctas][N]
     int64_t qs[3], os[3];
     int32_t batch, q_heads, rep, n_kv, n_q, n_tokens, causal;
+    int32_t cluster;                     // CTAs of the cluster that does a problem; 0: the line of tiles is cut into stretches
+    int32_t max_groups;                  // groups of query vectors of a request at most
 };
 
 // Where the problems of every request begin in the line of tiles.  A request of n query vectors (rep * its tokens) over t tiles has
@@ -194,24 +197,43 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
     cudaGridDependencySynchronize();
     // (the launch that joins the parts may come in as CTAs end: it waits for all of this one before it reads them)
     cudaTriggerProgrammaticLaunchCompletion();
-    const int64_t total = lay_line(a, N, prefix, reinterpret_cast<int64_t *>(smem));
-    const int ctas = stretches(total, gridDim.x);
-    if ((int)blockIdx.x >= ctas) return;
-    const int64_t begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
     const float logit_scale = (float)(1.4426950408889634 / sqrt((double)D));
-
-    int b = request_of(prefix, a.batch, begin);
+    int64_t begin = 0, end = 1;
+    int b = blockIdx.x / max(1, a.cluster * a.pool.kv_heads * a.max_groups);
+    if (!a.cluster) {
+        const int64_t total = lay_line(a, N, prefix, reinterpret_cast<int64_t *>(smem));
+        const int ctas = stretches(total, gridDim.x);
+        if ((int)blockIdx.x >= ctas) return;
+        begin = total * blockIdx.x / ctas;
+        end = total * (blockIdx.x + 1) / ctas;
+        b = request_of(prefix, a.batch, begin);
+    }
     for (int64_t f = begin; f < end;) {
-        while (prefix[b + 1] <= f) ++b;
+        if (!a.cluster)
+            while (prefix[b + 1] <= f) ++b;
         const Request rq = request_at(a, b, N);
-        const int64_t in_request = f - prefix[b];
-        const int problem = (int)(in_request / rq.places), place0 = (int)(in_request - (int64_t)problem * rq.places);
-        const int place1 = (int)min((int64_t)rq.places, place0 + (end - f));
+        int h, group, tile0, tile1;
         const bool first_segment = f == begin;
-        f += place1 - place0;
-        const int tile0 = max(0, place0 - A4_START), tile1 = place1 - A4_START;
-        if (tile1 <= tile0) continue;                            // (only what stands for a problem's beginning)
-        const int h = problem / rq.groups, group = problem - h * rq.groups;
+        if (a.cluster) {
+            // the tiles of a problem in equal shares; a CTA without any still takes part in the joining
+            f = end;
+            const int problem = blockIdx.x / a.cluster - b * a.pool.kv_heads * a.max_groups, rank = blockIdx.x % a.cluster;
+            h = problem / a.max_groups;
+            group = problem - h * a.max_groups;
+            if (group >= rq.groups) return;                      // (the whole cluster)
+            tile0 = (int)((int64_t)rq.tiles * rank / a.cluster);
+            tile1 = (int)((int64_t)rq.tiles * (rank + 1) / a.cluster);
+        } else {
+            const int64_t in_request = f - prefix[b];
+            const int problem = (int)(in_request / rq.places), place0 = (int)(in_request - (int64_t)problem * rq.places);
+            const int place1 = (int)min((int64_t)rq.places, place0 + (end - f));
+            f += place1 - place0;
+            tile0 = max(0, place0 - A4_START);
+            tile1 = place1 - A4_START;
+            if (tile1 <= tile0) continue;                        // (only what stands for a problem's beginning)
+            h = problem / rq.groups;
+            group = problem - h * rq.groups;
+        }
         const bool whole = tile0 == 0 && tile1 == rq.tiles;
         const int vec0 = group * N;                              // vector v of the group is token (vec0 + v) / rep, head h rep + (vec0 + v) % rep
         const int vectors = min(N, rq.tokens * a.rep - vec0);
@@ -629,7 +651,38 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
 #pragma unroll
                 for (int e = 0; e < EACH; ++e) acc[e] = fmaf(from[sub + e * PER], share, acc[e]);
             }
-            if (whole) {
+            if (a.cluster > 1) {
+                // joined among the cluster's CTAs in their order: each leaves its sums in its shared memory and takes a share of the numbers
+                __syncthreads();
+                float *sums = reinterpret_cast<float *>(smem);
+                float2 *own = reinterpret_cast<float2 *>(ml);
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) sums[v * D + sub + e * PER] = acc[e];
+                if (sub == 0) own[v] = make_float2(m, den);
+                namespace cg = cooperative_groups;
+                cg::cluster_group cluster = cg::this_cluster();
+                cluster.sync();
+                const int share_of = N * D / a.cluster, x0 = (int)(blockIdx.x % a.cluster) * share_of;
+                for (int x = x0 + threadIdx.x; x < x0 + share_of; x += A4_THREADS) {
+                    const int vx = x / D;
+                    float mx = -INFINITY, dx = 0.f, ox = 0.f;
+#pragma unroll 4
+                    for (int i = 0; i < a.cluster; ++i) mx = fmaxf(mx, cluster.map_shared_rank(own, i)[vx].x);
+#pragma unroll 4
+                    for (int i = 0; i < a.cluster; ++i) {
+                        const float2 part = cluster.map_shared_rank(own, i)[vx];
+                        const float share = part.x == -INFINITY ? 0.f : exp2_fast(part.x - mx);
+                        dx = fmaf(part.y, share, dx);
+                        ox = fmaf(cluster.map_shared_rank(sums, i)[x], share, ox);
+                    }
+                    if (vx < vectors) {
+                        const int vv = vec0 + vx, tok = vv / a.rep, head = h * a.rep + vv % a.rep;
+                        T *to = (T *)a.o + (a.cu ? (int64_t)(rq.first_token + tok) * a.os[2] : b * a.os[0] + tok * a.os[2]) + head * a.os[1];
+                        store_from(to, x % D, dx == 0.f ? 0.f : ox / dx);
+                    }
+                }
+                cluster.sync();                                  // (nobody leaves while its shared memory is read)
+            } else if (whole) {
                 if (v < vectors) {
                     const int vv = vec0 + v, tok = vv / a.rep, head = h * a.rep + vv % a.rep;
                     T *to = (T *)a.o + (a.cu ? (int64_t)(rq.first_token + tok) * a.os[2] : b * a.os[0] + tok * a.os[2]) + head * a.os[1];
@@ -736,7 +789,7 @@ __global__ void __launch_bounds__(A4_MERGE_THREADS) attend4_merge_kernel(const _
 
 constexpr int A4_MAX_CTAS_PER_SM = 8;    // what the workspace has room for
 
-template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_form(const Attend4Args &a, cudaStream_t st)
+template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_form(Attend4Args a, cudaStream_t st)
 {
     using C = A4<D, NT, PARTS>;
     auto kern = attend4_kernel<T, D, NT, PARTS, LIST>;
@@ -753,9 +806,44 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
         per_sm = per_sm < 1 ? 1 : (per_sm > A4_MAX_CTAS_PER_SM ? A4_MAX_CTAS_PER_SM : per_sm);
         if (dev < 64) known[dev][big].store(per_sm, std::memory_order_relaxed);
     }
-    const int max_groups = (int)(((int64_t)a.n_q * a.rep + C::N - 1) / C::N);
+    a.max_groups = (int)(((int64_t)a.n_q * a.rep + C::N - 1) / C::N);
+    const int max_groups = a.max_groups;
     const int64_t problems = (int64_t)a.batch * a.pool.kv_heads * max_groups;
-    if (problems > 0x7fffffff) return ELM_ERR_SHAPE;
+    if (problems > 0x7fffffff / 16) return ELM_ERR_SHAPE;
+    // Short problems, so few that a cluster for each is resident at once, are done in one launch: as many CTAs as give a warp two tiles (at
+    // most 16 CTAs with up to four tiles a warp); a single CTA each where they have no more than 8 tiles.
+    const int tiles = (a.n_kv + A4_TILE - 1) / A4_TILE;
+    for (int size = 1; size <= 16; size *= 2) {
+        if (tiles > size * A4_WARPS * (size == 16 ? 4 : 2)) continue;
+        if (size > 1) {
+            static std::atomic<int> resident[64][5];
+            const int at = size == 2 ? 0 : size == 4 ? 1 : size == 8 ? 2 : 3;
+            int clusters = dev < 64 ? resident[dev][at].load(std::memory_order_relaxed) : 0;
+            if (clusters == 0) {
+                clusters = resident_clusters(kern, A4_THREADS, smem, size) + 1;       // (+ 1: 0 is not known yet)
+                ELM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::total(A4_MAX_BATCH)));
+                if (dev < 64) resident[dev][at].store(clusters, std::memory_order_relaxed);
+            }
+            if (problems > clusters - 1) continue;
+        }
+        a.cluster = size;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)size;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(problems * size));
+        cfg.blockDim = dim3(A4_THREADS);
+        cfg.dynamicSmemBytes = (size_t)smem;
+        cfg.stream = st;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        ELM_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, a));
+        count_launches(1);
+        return cuda_status(cudaGetLastError());
+    }
     // no more CTAs than the longest line of tiles has stretches
     const int64_t places = problems * (A4_START + (a.n_kv + A4_TILE - 1) / A4_TILE);
     const int grid = stretches(places, per_sm * device_sm_count());
