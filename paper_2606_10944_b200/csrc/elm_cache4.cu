@@ -8,8 +8,8 @@
 namespace elm {
 namespace {
 
-constexpr int APP_THREADS = 256;
-constexpr int APP_TILE = 32;             // tokens of a CTA at most
+constexpr int APP_THREADS = ROPE_THREADS;
+constexpr int APP_TILE = 32;             // tokens of a CTA at most (number by number)
 
 struct AppendArgs {
     const void *q, *k, *v;
@@ -17,8 +17,10 @@ struct AppendArgs {
     const int32_t *positions, *slots;
     unsigned char *rows;
     int64_t qs[2], ks[2], vs[2], qos[2];
+    RopeShape query;                     // of the CTAs that turn queries
     double scale;
     int32_t n_tokens, q_heads, kv_heads, rotary, page_shift, tile;
+    int32_t q_ctas;                      // CTAs from 0 on that turn queries; the others store rows
     uint32_t n_slots;
 };
 
@@ -78,14 +80,115 @@ __device__ __forceinline__ void rotate_group(const T *row, int first, int rotary
     }
 }
 
-// A thread takes a group of 16 numbers: of a query (rotated, stored as it is), a key or a value (made a code).  The groups of a row are
-// neighbouring lanes, so that a row's codes leave in one piece; four lanes put their scales together.
-template <typename T, int D, bool WIDE, bool HALVES>
+// Queries are turned by the first CTAs as elm_rope does it; the others store rows, a thread two groups of 16 numbers: of a key that
+// is rotated in halves both halves of its pairs.  The groups of a row are neighbouring lanes, so that its codes leave in one piece.
+template <typename T, int D, bool HALVES>
 __global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTurns turns)
 {
     using R = Row4<D>;
+    constexpr int G = R::GROUPS, E = 16 / (int)sizeof(T), HALF = G / 2;
+    extern __shared__ __align__(16) float cs[];
+    cudaGridDependencySynchronize();
+    if ((int)blockIdx.x < a.q_ctas) {
+        const int64_t t0 = (int64_t)blockIdx.x * a.query.tile;
+        rope_rows<T, E, HALVES>((const T *)a.q, (T *)a.q_out, a.query, turns, t0, min(a.query.tile, a.n_tokens - (int)t0), cs,
+                                [&](int64_t t, int64_t &from, int64_t &to, int64_t &pos) {
+                                    from = t * a.qs[0];
+                                    to = t * a.qos[0];
+                                    pos = a.rotary ? a.positions[t] : 0;
+                                    return (uint32_t)a.slots[t] < a.n_slots;
+                                });
+        return;
+    }
+    // a token: 2 kv_heads rows of numbers (keys, values), G / 2 threads each
+    const int pairs = a.rotary / 2, row_cs = rope_cs_floats<16>(pairs);
+    const int t0 = ((int)blockIdx.x - a.q_ctas) * a.tile;
+    const int count = min(a.tile, a.n_tokens - t0);
+    for (int i = threadIdx.x; i < count * pairs; i += APP_THREADS) {
+        const int t = i / pairs, p = i - t * pairs;
+        *reinterpret_cast<float2 *>(cs + t * row_cs + 2 * p + 4 * (p / 16)) = rope_cos_sin(a.positions[t0 + t], turns.turn[p], a.scale, a.scale);
+    }
+    __syncthreads();
+    const int total = count * a.kv_heads * G;                    // items: (token, head, key or value, pair of groups)
+    for (int i0 = threadIdx.x & ~31; i0 < total; i0 += APP_THREADS) {
+        const int i = i0 + (threadIdx.x & 31);
+        const bool live = i < total;
+        const int j = i % G, th = live ? i / G : 0, t = th / a.kv_heads, h = th - t * a.kv_heads;
+        const uint32_t slot = (uint32_t)a.slots[t0 + t];
+        const bool there = live && slot < a.n_slots;
+        const bool key = j < HALF;
+        const int p = key ? j : j - HALF;
+        // the two groups: halves of pairs while they are rotated in halves, else side by side
+        const int turned = key ? a.rotary / C4_GROUP : 0;        // groups that are rotated
+        const bool halves = HALVES && 2 * p < turned;
+        const int g0 = halves ? p : 2 * p, g1 = halves ? p + turned / 2 : 2 * p + 1;
+        uint32_t byte0 = 0, byte1 = 0;
+        unsigned char *row = nullptr;
+        if (there) {
+            const T *src = key ? (const T *)a.k + (int64_t)(t0 + t) * a.ks[0] + h * a.ks[1] : (const T *)a.v + (int64_t)(t0 + t) * a.vs[0] + h * a.vs[1];
+            float x[C4_GROUP], y[C4_GROUP];
+            load_group<T, true>(src, g0 * C4_GROUP, x);
+            load_group<T, true>(src, g1 * C4_GROUP, y);
+            if (halves) {
+                const float *c = cs + t * row_cs + p * 36;
+#pragma unroll
+                for (int e = 0; e < C4_GROUP; e += 2) {
+                    const float4 v = *reinterpret_cast<const float4 *>(c + 2 * e);
+                    rope_turn(x[e], y[e], make_float2(v.x, v.y));
+                    rope_turn(x[e + 1], y[e + 1], make_float2(v.z, v.w));
+                }
+            } else if (!HALVES && g0 < turned) {                 // (rotary is a multiple of 32: both groups or none)
+                const float *c = cs + t * row_cs + p * 36;
+#pragma unroll
+                for (int e = 0; e < C4_GROUP; e += 4) {
+                    const float4 v = *reinterpret_cast<const float4 *>(c + e), w = *reinterpret_cast<const float4 *>(c + 16 + e);
+                    rope_turn(x[e], x[e + 1], make_float2(v.x, v.y));
+                    rope_turn(x[e + 2], x[e + 3], make_float2(v.z, v.w));
+                    rope_turn(y[e], y[e + 1], make_float2(w.x, w.y));
+                    rope_turn(y[e + 2], y[e + 3], make_float2(w.z, w.w));
+                }
+            }
+            uint2 c0, c1;
+            byte0 = quantise4(x, c0);
+            byte1 = quantise4(y, c1);
+            const uint32_t page = slot >> a.page_shift, in_page = slot & ((1u << a.page_shift) - 1u);
+            row = a.rows + ((((uint64_t)page * (uint32_t)a.kv_heads + h) << a.page_shift) + in_page) * R::BYTES;
+            uint2 *codes = reinterpret_cast<uint2 *>(row + (key ? 0 : R::CODES));
+            codes[g0] = c0;
+            codes[g1] = c1;
+        }
+        // scales of the row's key or value: this thread's two, and its neighbours', as words
+        uint32_t w0 = 0, w1 = 0;                                 // scales of groups 0 .. 3 and 4 .. 7
+        if (g0 < 4) w0 |= byte0 << (8 * g0);
+        else w1 |= byte0 << (8 * (g0 - 4));
+        if (g1 < 4) w0 |= byte1 << (8 * g1);
+        else w1 |= byte1 << (8 * (g1 - 4));
+#pragma unroll
+        for (int o = 1; o < HALF; o <<= 1) {
+            w0 |= __shfl_xor_sync(0xffffffffu, w0, o);
+            if (G == 8) w1 |= __shfl_xor_sync(0xffffffffu, w1, o);
+        }
+        if (row && p == 0) {
+            unsigned char *scales = row + R::SCALES + (key ? 0 : G);
+            if (G == 8) {
+                *reinterpret_cast<uint2 *>(scales) = make_uint2(w0, w1);
+            } else {
+                *reinterpret_cast<uint32_t *>(scales) = w0;
+                *reinterpret_cast<uint32_t *>(row + R::SCALES + 2 * G + (key ? 0 : 4)) = 0u;       // (the unused bytes)
+            }
+        }
+    }
+}
+
+// Rows whose numbers are not on 16-byte boundaries, or of which a part is rotated that does not end with a group: a thread takes a group of 16
+// numbers of a query, a key or a value.
+template <typename T, int D, bool WIDE, bool HALVES>
+__global__ void __launch_bounds__(APP_THREADS) append4_any_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTurns turns)
+{
+    using R = Row4<D>;
     constexpr int G = R::GROUPS;
-    extern __shared__ float2 cs[];                             // [tile][rotary / 2]
+    extern __shared__ __align__(16) float cs_floats[];
+    float2 *cs = reinterpret_cast<float2 *>(cs_floats);        // [tile][rotary / 2]
     cudaGridDependencySynchronize();
     const int pairs = a.rotary / 2;
     const int t0 = blockIdx.x * a.tile;
@@ -199,59 +302,105 @@ struct ReadArgs {
     int64_t rows;                        // batch * kv_heads * n
 };
 
-// A thread makes 8 numbers (4 bytes of codes): 16 bytes of bf16, so that a warp's stores are whole lines.
+// A warp takes 32 rows, whose places its lanes look up side by side, and makes one (d = 64: two) at a time: a lane 8 numbers, from 4 bytes of
+// codes, so that its stores are whole lines.
+constexpr int READ_AHEAD = 8;            // rows (pairs of rows) requested together
 template <typename T, int D> __global__ void __launch_bounds__(256) read4_kernel(const __grid_constant__ ReadArgs a)
 {
     using R = Row4<D>;
-    constexpr int PER_ROW = 2 * D / 8;
+    constexpr int AT_ONCE = 128 / D, LANES = 32 / AT_ONCE;       // rows of a step, lanes of a row
     cudaGridDependencySynchronize();
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t out_row = i / PER_ROW;
-    if (out_row >= a.rows) return;
-    const int j = (int)(i % PER_ROW);
-    const int64_t problem = out_row / a.n;
-    const int64_t e = out_row - problem * a.n;
-    const int b = (int)(problem / a.pool.kv_heads), h = (int)(problem - (int64_t)b * a.pool.kv_heads);
-    const int64_t r = a.idx ? a.idx[out_row] : e;
-    uint32_t row = r < 0 || (a.length && r >= a.length[b]) ? NO_ROW : pool_row(a.pool, b, h, r);
-    uint32_t half2s[4] = {0u, 0u, 0u, 0u};
-    if (row != NO_ROW) {
-        const unsigned char *p = a.pool.rows + (uint64_t)row * R::BYTES;
-        const uint32_t codes = *reinterpret_cast<const uint32_t *>(p + 4 * j);
-        const uint32_t s = scale4_half_bits(p[R::SCALES + j / 2]) * 0x10001u;
-        codes8_to_half2(codes, half2s);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) half2s[k] = hmul2_bits(half2s[k], s);
+    const int lane = threadIdx.x & 31;
+    const int64_t first = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * 32;
+    if (first >= a.rows) return;
+    uint32_t place = NO_ROW;
+    if (first + lane < a.rows) {
+        const int64_t out_row = first + lane, problem = out_row / a.n, e = out_row - problem * a.n;
+        const int b = (int)(problem / a.pool.kv_heads), h = (int)(problem - (int64_t)b * a.pool.kv_heads);
+        const int64_t r = a.idx ? a.idx[out_row] : e;
+        if (r >= 0 && (!a.length || r < a.length[b])) place = pool_row(a.pool, b, h, r);
     }
-    T *out = (T *)(j < PER_ROW / 2 ? a.k : a.v) + out_row * D + (j % (PER_ROW / 2)) * 8;
-    constexpr int E = 16 / (int)sizeof(T);
+    const int j = lane % LANES;
+    const bool key = j < LANES / 2;
+    T *out = (T *)(key ? a.k : a.v) + (j % (LANES / 2)) * 8;
+    const int64_t left = a.rows - first;
 #pragma unroll
-    for (int k = 0; k < 8; k += E) {
-        Chunk<T, E> c;
+    for (int s0 = 0; s0 < 32 / AT_ONCE; s0 += READ_AHEAD) {
+        uint32_t codes[READ_AHEAD], scale[READ_AHEAD];
 #pragma unroll
-        for (int x = 0; x < E; x += 2) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&half2s[(k + x) / 2]));
-            c.v[x] = f.x;
-            c.v[x + 1] = f.y;
+        for (int s = 0; s < READ_AHEAD; ++s) {
+            const uint32_t row = __shfl_sync(0xffffffffu, place, (s0 + s) * AT_ONCE + lane / LANES);
+            codes[s] = scale[s] = 0;
+            if (row != NO_ROW) {
+                const unsigned char *p = a.pool.rows + (uint64_t)row * R::BYTES;
+                codes[s] = *reinterpret_cast<const uint32_t *>(p + 4 * j);
+                scale[s] = p[R::SCALES + j / 2];
+            }
         }
-        c.store(out + k);
+#pragma unroll
+        for (int s = 0; s < READ_AHEAD; ++s) {
+            const int at = (s0 + s) * AT_ONCE + lane / LANES;
+            uint32_t half2s[4];
+            codes8_to_half2(codes[s], half2s);
+            const uint32_t sc = scale4_half_bits(scale[s]) * 0x10001u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) half2s[k] = hmul2_bits(half2s[k], sc);
+            if (at >= left) continue;
+            constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+            for (int k = 0; k < 8; k += E) {
+                Chunk<T, E> c;
+#pragma unroll
+                for (int x = 0; x < E; x += 2) {
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&half2s[(k + x) / 2]));
+                    c.v[x] = f.x;
+                    c.v[x + 1] = f.y;
+                }
+                c.store(out + (first + at) * D + k);
+            }
+        }
     }
 }
 
 template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &turns, bool halves, bool wide, cudaStream_t st)
 {
-    const int per_token = (2 * a.kv_heads + a.q_heads) * (D / C4_GROUP);
-    // tokens per CTA: two rounds of its threads (a token's cosines are formed once for all its heads), fewer where the tokens would
-    // not fill the GPU
-    int tile = (2 * APP_THREADS + per_token - 1) / per_token;
-    const int fill = a.n_tokens / (4 * device_sm_count());
-    if (tile > fill) tile = fill < 1 ? 1 : fill;
-    if (tile > APP_TILE) tile = APP_TILE;
-    a.tile = tile;
-    const size_t smem = (size_t)tile * (a.rotary / 2) * sizeof(float2);
-    const dim3 grid((unsigned)(((int64_t)a.n_tokens + tile - 1) / tile));
-    auto kern = wide ? (halves ? append4_kernel<T, D, true, true> : append4_kernel<T, D, true, false>)
-                     : (halves ? append4_kernel<T, D, false, true> : append4_kernel<T, D, false, false>);
+    const int sms = device_sm_count();
+    const int fill = a.n_tokens / (4 * sms);                     // tokens per CTA that would still fill the GPU
+    auto tile_of = [&](int per_token) {
+        int tile = (2 * APP_THREADS + per_token - 1) / per_token;
+        if (tile > fill) tile = fill < 1 ? 1 : fill;
+        return tile > APP_TILE ? APP_TILE : tile;
+    };
+    const int pairs = a.rotary / 2;
+    if (wide && a.rotary % 32 == 0) {
+        constexpr int E = 16 / (int)sizeof(T);
+        int64_t q_ctas = 0;
+        size_t smem = 0;
+        a.query = RopeShape{a.q_heads, a.rotary, 0, 0, 0, 0, a.qs[1], a.qos[1], a.scale, a.scale};
+        if (a.q_heads > 0) {
+            // in place, numbers that are not rotated stay
+            a.query.per_head = pairs / E + (a.q == a.q_out ? 0 : (D - a.rotary) / E);
+            if (a.query.per_head > 0) {
+                rope_share(a.query, a.n_tokens, sms);
+                q_ctas = (a.n_tokens + a.query.tile - 1) / a.query.tile;
+                smem = (size_t)a.query.tile * rope_cs_floats<E>(pairs) * sizeof(float);
+            }
+        }
+        a.tile = tile_of(a.kv_heads * (D / C4_GROUP));
+        const size_t rows_smem = (size_t)a.tile * rope_cs_floats<16>(pairs) * sizeof(float);
+        if (rows_smem > smem) smem = rows_smem;
+        const int64_t ctas = q_ctas + (a.n_tokens + a.tile - 1) / a.tile;
+        if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
+        a.q_ctas = (int)q_ctas;
+        ELM_CUDA_TRY(launch_after(halves ? append4_kernel<T, D, true> : append4_kernel<T, D, false>, dim3((unsigned)ctas), dim3(APP_THREADS), smem, st, a, turns));
+        count_launches(1);
+        return cuda_status(cudaGetLastError());
+    }
+    a.tile = tile_of((2 * a.kv_heads + a.q_heads) * (D / C4_GROUP));
+    const size_t smem = (size_t)a.tile * pairs * sizeof(float2);
+    const dim3 grid((unsigned)(((int64_t)a.n_tokens + a.tile - 1) / a.tile));
+    auto kern = wide ? (halves ? append4_any_kernel<T, D, true, true> : append4_any_kernel<T, D, true, false>)
+                     : (halves ? append4_any_kernel<T, D, false, true> : append4_any_kernel<T, D, false, false>);
     ELM_CUDA_TRY(launch_after(kern, grid, dim3(APP_THREADS), smem, st, a, turns));
     count_launches(1);
     return cuda_status(cudaGetLastError());
@@ -344,7 +493,7 @@ extern "C" int elm_cache4_read(const void *rows, const int32_t *table, const int
     a.v = V_out;
     a.n = p->n_kv;
     a.rows = (int64_t)p->batch * p->kv_heads * p->n_kv;
-    const int64_t ctas = (a.rows * (2 * p->d / 8) + 255) / 256;
+    const int64_t ctas = (a.rows + 255) / 256;
     if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
     auto kern = p->dtype == ELM_BF16 ? (p->d == 64 ? read4_kernel<__nv_bfloat16, 64> : read4_kernel<__nv_bfloat16, 128>)
                                      : (p->d == 64 ? read4_kernel<float, 64> : read4_kernel<float, 128>);

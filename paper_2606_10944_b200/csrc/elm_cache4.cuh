@@ -81,17 +81,28 @@ __device__ __forceinline__ uint32_t hmul2_bits(uint32_t a, uint32_t b)
 // x / scale is formed from the correctly rounded reciprocal r by q = x r, q + r (x - q scale): correctly rounded for every quotient that
 // matters (Markstein 1990), so that a number halfway between two codes is seen as that - a product with the rounded reciprocal
 // alone would put half of those to the wrong side, and of bf16 numbers one in a hundred is a tie.
-__device__ __forceinline__ uint32_t quantise4(const float (&x)[C4_GROUP], uint2 &codes)
+__device__ __forceinline__ float max_nan(float a, float b)      // NaN if either is
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t quantise4(float (&x)[C4_GROUP], uint2 &codes)
 {
     constexpr float LARGEST = 61440.f;
-    float top = 0.f;
-    bool nan = false;
+    float top = fabsf(x[0]);
 #pragma unroll
-    for (int i = 0; i < C4_GROUP; ++i) {
-        top = fmaxf(top, fabsf(x[i]));
-        nan |= x[i] != x[i];
+    for (int i = 1; i < C4_GROUP; ++i) top = max_nan(top, fabsf(x[i]));
+    if (!(top <= LARGEST)) {
+        if (top != top) {
+            codes = make_uint2(0u, 0u);
+            return 0xffu;                                                       // fp16 NaN times any code
+        }
+#pragma unroll
+        for (int i = 0; i < C4_GROUP; ++i) x[i] = fminf(fmaxf(x[i], -LARGEST), LARGEST);
+        top = LARGEST;
     }
-    const float q = __fdiv_rn(fminf(top, LARGEST), 6.f);
+    const float q = __fdiv_rn(top, 6.f);
     uint32_t byte;
     if (q >= 0x1p-14f) {
         const uint32_t u = __float_as_uint(q);
@@ -107,19 +118,14 @@ __device__ __forceinline__ uint32_t quantise4(const float (&x)[C4_GROUP], uint2 
         float y[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const float v = fminf(fmaxf(x[i + k], -LARGEST), LARGEST);          // (infinities: the quotient's correction would be NaN)
-            const float y0 = v * r;
-            y[k] = copysignf(fmaf(fmaf(-y0, s, v), r, y0), v);                  // (-0 stays -0)
+            const float y0 = x[i + k] * r;
+            y[k] = copysignf(fmaf(fmaf(-y0, s, x[i + k]), r, y0), x[i + k]);    // (-0 stays -0)
         }
         uint32_t two;
         asm("{\n\t.reg .b8 b;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %1, %2;\n\tcvt.u32.u8 %0, b;\n\t}" : "=r"(two) : "f"(y[1]), "f"(y[0]));
         w[i >> 3] |= two << (4 * (i & 7));
     }
     codes = make_uint2(w[0], w[1]);
-    if (nan) {
-        codes = make_uint2(0u, 0u);
-        return 0xffu;                                                           // fp16 NaN times any code
-    }
     return byte;
 }
 

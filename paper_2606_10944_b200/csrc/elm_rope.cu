@@ -2,127 +2,50 @@
 //
 //   a' = a c - b s,  b' = b c + a s,  (c, s) = scale (cos, sin)(position * inv_freq[i])
 //
-// One pass over X: HBM-bound (2 d numbers moved per head and token).  A CTA takes a few tokens: its threads first form the
-// tokens' cosines and sines once for all heads (fp64, see elm_rope.cuh), then walk over (token, head, chunk), 16 bytes of each half of
-// a pair per thread.
+// One pass over X: HBM-bound (2 d numbers moved per head and token).  A CTA takes a few tokens; cosines and sines are formed once for all heads
+// of a token (fp64, see elm_rope.cuh).
 #include "elm_rope.cuh"
 
 namespace elm {
 namespace {
-
-constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_TILE = 128;           // tokens of a CTA at most
-constexpr int ROPE_UNROLL = 4;           // chunks (pairs of chunks) a thread has in flight
 
 struct RopeArgs {
     const void *x;
     void *out;
     const int32_t *positions;
     int64_t first;
-    int64_t xs[3], os[3];
-    double scale, sin_scale;
-    int32_t heads, n_tokens, d, rotary, tile, copy_chunks;
+    int64_t xs[2], os[2];                // batch, token
+    RopeShape shape;
+    int32_t n_tokens;
     int64_t tokens;                      // batch * n_tokens
 };
 
-// HALVES: item j < rotary / 2 / E holds numbers [E j, E j + E) and their partners rotary / 2 further on.  PAIRS: item j holds
-// 2 E numbers side by side.  Items from there on copy E numbers (copy_chunks of them; none when out is X).
 template <typename T, int E, bool HALVES>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeTurns turns)
+__global__ void __launch_bounds__(ROPE_THREADS, 3) rope_kernel(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeTurns turns)
 {
-    __shared__ int64_t row_of[ROPE_TILE][2];                   // a token's first row in X and in out
-    extern __shared__ float2 cs[];                             // [tile][rotary / 2]
-    const int pairs = a.rotary / 2;
-    const int64_t t0 = (int64_t)blockIdx.x * a.tile;
-    const int count = (int)(a.tokens - t0 < a.tile ? a.tokens - t0 : a.tile);
-    for (int i = threadIdx.x; i < count * pairs; i += ROPE_THREADS) {
-        const int t = i / pairs, p = i - t * pairs;
-        const int64_t pos = a.positions ? (int64_t)a.positions[t0 + t] : a.first + (t0 + t) % a.n_tokens;
-        cs[i] = rope_cos_sin(pos, turns.turn[p], a.scale, a.sin_scale);
-    }
-    for (int t = threadIdx.x; t < count; t += ROPE_THREADS) {
-        const int64_t b = (t0 + t) / a.n_tokens, n = (t0 + t) - b * a.n_tokens;
-        row_of[t][0] = b * a.xs[0] + n * a.xs[2];
-        row_of[t][1] = b * a.os[0] + n * a.os[2];
-    }
-    __syncthreads();
-    const int turn_items = pairs / E;
-    const int per_head = turn_items + a.copy_chunks;
-    const int per_token = per_head * a.heads;
-    const int total = count * per_token;
-    const T *x = (const T *)a.x;
-    T *out = (T *)a.out;
-    for (int i0 = threadIdx.x; i0 < total; i0 += ROPE_THREADS * ROPE_UNROLL) {
-        Chunk<T, E> u[ROPE_UNROLL], w[ROPE_UNROLL];
-        int64_t to[ROPE_UNROLL];
-        int kind[ROPE_UNROLL];                                 // first pair of the item, -1: copied, -2: none
-#pragma unroll
-        for (int k = 0; k < ROPE_UNROLL; ++k) {
-            const int i = i0 + k * ROPE_THREADS;
-            kind[k] = -2;
-            if (i < total) {
-                const int t = i / per_token, r = i - t * per_token;
-                const int h = r / per_head, j = r - h * per_head;
-                const int64_t from = row_of[t][0] + h * a.xs[1];
-                to[k] = row_of[t][1] + h * a.os[1];
-                if (j < turn_items) {
-                    kind[k] = t * pairs + j * E;
-                    const int o = HALVES ? j * E : 2 * j * E;
-                    to[k] += o;
-                    u[k].load(x + from + o);
-                    w[k].load(x + from + o + (HALVES ? pairs : E));
-                } else {
-                    kind[k] = -1;
-                    const int o = a.rotary + (j - turn_items) * E;
-                    to[k] += o;
-                    u[k].load(x + from + o);
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < ROPE_UNROLL; ++k) {
-            if (kind[k] >= 0) {
-                const float2 *c = cs + kind[k];
-                if constexpr (HALVES) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) rope_turn(u[k].v[e], w[k].v[e], c[e]);
-                } else if constexpr (E == 1) {
-                    rope_turn(u[k].v[0], w[k].v[0], c[0]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; e += 2) {
-                        rope_turn(u[k].v[e], u[k].v[e + 1], c[e / 2]);
-                        rope_turn(w[k].v[e], w[k].v[e + 1], c[E / 2 + e / 2]);
-                    }
-                }
-                u[k].store(out + to[k]);
-                w[k].store(out + to[k] + (HALVES ? pairs : E));
-            } else if (kind[k] == -1) {
-                u[k].store(out + to[k]);
-            }
-        }
-    }
+    extern __shared__ __align__(16) float cs[];
+    cudaGridDependencySynchronize();
+    const int64_t t0 = (int64_t)blockIdx.x * a.shape.tile;
+    const int count = (int)(a.tokens - t0 < a.shape.tile ? a.tokens - t0 : a.shape.tile);
+    rope_rows<T, E, HALVES>((const T *)a.x, (T *)a.out, a.shape, turns, t0, count, cs, [&](int64_t t, int64_t &from, int64_t &to, int64_t &pos) {
+        const uint32_t b = (uint32_t)t / (uint32_t)a.n_tokens, n = (uint32_t)t - b * (uint32_t)a.n_tokens;
+        from = b * a.xs[0] + n * a.xs[1];
+        to = b * a.os[0] + n * a.os[1];
+        pos = a.positions ? (int64_t)a.positions[t] : a.first + n;
+        return true;
+    });
 }
 
-template <typename T, int E> int launch_rope(RopeArgs &a, const RopeTurns &turns, bool halves, bool in_place, cudaStream_t st)
+template <typename T, int E> int launch_rope(RopeArgs &a, int d, const RopeTurns &turns, bool halves, bool in_place, cudaStream_t st)
 {
-    a.copy_chunks = in_place ? 0 : (a.d - a.rotary) / E;
-    const int pairs = a.rotary / 2;
-    // tokens per CTA: about two rounds of its threads' chunks (cosines of a token cost as much as a few chunks, so that one
-    // token of one head alone is dear), as few as that where the tokens would not fill the GPU
-    const int per_token = (pairs / E + a.copy_chunks) * a.heads;
-    int tile = (2 * ROPE_THREADS * ROPE_UNROLL + per_token - 1) / per_token;
-    const int64_t fill = a.tokens / (4 * (int64_t)device_sm_count());
-    if (tile > fill) tile = fill < 1 ? 1 : (int)fill;
-    const int most = 32768 / (pairs * (int)sizeof(float2));
-    if (tile > most) tile = most;
-    if (tile > ROPE_TILE) tile = ROPE_TILE;
-    a.tile = tile;
-    const int64_t ctas = (a.tokens + tile - 1) / tile;
+    const int pairs = a.shape.rotary / 2;
+    a.shape.per_head = pairs / E + (in_place ? 0 : (d - a.shape.rotary) / E);
+    rope_share(a.shape, a.tokens, device_sm_count());
+    const int64_t ctas = (a.tokens + a.shape.tile - 1) / a.shape.tile;
     if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
-    const size_t smem = (size_t)tile * pairs * sizeof(float2);
-    if (halves) rope_kernel<T, E, true><<<(unsigned)ctas, ROPE_THREADS, smem, st>>>(a, turns);
-    else rope_kernel<T, E, false><<<(unsigned)ctas, ROPE_THREADS, smem, st>>>(a, turns);
+    const size_t smem = (size_t)a.shape.tile * rope_cs_floats<E>(pairs) * sizeof(float);
+    auto kern = halves ? rope_kernel<T, E, true> : rope_kernel<T, E, false>;
+    ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)ctas), dim3(ROPE_THREADS), smem, st, a, turns));
     count_launches(1);
     return cuda_status(cudaGetLastError());
 }
@@ -147,18 +70,18 @@ extern "C" int elm_rope(const void *X, const int32_t *positions, int64_t first_p
     if (!rope_turns(p->inv_freq, p->rotary_dim / 2, turns)) return ELM_ERR_SHAPE;
     RopeArgs a;
     const int64_t dense[3] = {(int64_t)p->heads * p->n_tokens * p->d, (int64_t)p->n_tokens * p->d, p->d};
-    int64_t all = 0;
+    int64_t xs[3], os[3], all = 0;
     for (int i = 0; i < 3; ++i) {
-        a.xs[i] = zeros(p->x_stride) ? dense[i] : p->x_stride[i];
-        a.os[i] = zeros(p->out_stride) ? dense[i] : p->out_stride[i];
-        all |= a.xs[i] | a.os[i];
+        xs[i] = zeros(p->x_stride) ? dense[i] : p->x_stride[i];
+        os[i] = zeros(p->out_stride) ? dense[i] : p->out_stride[i];
+        all |= xs[i] | os[i];
     }
     // rows of out that would be written twice
-    if ((p->batch > 1 && a.os[0] == 0) || (p->heads > 1 && a.os[1] == 0) || (p->n_tokens > 1 && a.os[2] == 0)) return ELM_ERR_SHAPE;
+    if ((p->batch > 1 && os[0] == 0) || (p->heads > 1 && os[1] == 0) || (p->n_tokens > 1 && os[2] == 0)) return ELM_ERR_SHAPE;
     const bool in_place = X == out;
     if (in_place)
         for (int i = 0; i < 3; ++i)
-            if (a.xs[i] != a.os[i]) return ELM_ERR_SHAPE;
+            if (xs[i] != os[i]) return ELM_ERR_SHAPE;
     const int item = (int)elt_bytes(p->dtype);
     if (((uintptr_t)X | (uintptr_t)out) & (item - 1)) return ELM_ERR_ALIGN;
     if (positions && ((uintptr_t)positions & 3)) return ELM_ERR_ALIGN;
@@ -166,12 +89,12 @@ extern "C" int elm_rope(const void *X, const int32_t *positions, int64_t first_p
     a.out = out;
     a.positions = positions;
     a.first = first_position;
-    a.scale = p->scale;
-    a.sin_scale = p->inverse ? -p->scale : p->scale;
-    a.heads = p->heads;
+    for (int i = 0; i < 2; ++i) {
+        a.xs[i] = xs[2 * i];
+        a.os[i] = os[2 * i];
+    }
+    a.shape = RopeShape{p->heads, p->rotary_dim, 0, 0, 0, 0, xs[1], os[1], p->scale, p->inverse ? -p->scale : p->scale};
     a.n_tokens = p->n_tokens;
-    a.d = p->d;
-    a.rotary = p->rotary_dim;
     a.tokens = (int64_t)p->batch * p->n_tokens;
     cudaStream_t st = (cudaStream_t)stream;
     const bool halves = p->layout == ELM_ROPE_HALVES;
@@ -179,8 +102,8 @@ extern "C" int elm_rope(const void *X, const int32_t *positions, int64_t first_p
     const int E = 16 / item;
     const bool wide = !(((uintptr_t)X | (uintptr_t)out) & 15) && all % E == 0 && p->d % E == 0 && p->rotary_dim / 2 % E == 0;
     if (p->dtype == ELM_BF16)
-        return wide ? launch_rope<__nv_bfloat16, 8>(a, turns, halves, in_place, st) : launch_rope<__nv_bfloat16, 1>(a, turns, halves, in_place, st);
-    return wide ? launch_rope<float, 4>(a, turns, halves, in_place, st) : launch_rope<float, 1>(a, turns, halves, in_place, st);
+        return wide ? launch_rope<__nv_bfloat16, 8>(a, p->d, turns, halves, in_place, st) : launch_rope<__nv_bfloat16, 1>(a, p->d, turns, halves, in_place, st);
+    return wide ? launch_rope<float, 4>(a, p->d, turns, halves, in_place, st) : launch_rope<float, 1>(a, p->d, turns, halves, in_place, st);
 }
 
 extern "C" int elm_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double original, double low, double high,

@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include "elm_common.cuh"
+#include "elm_sm100.cuh"
 
 namespace elm {
 
@@ -93,5 +94,171 @@ template <typename T, int E> struct Chunk {
         }
     }
 };
+
+// A CTA's share of a rotation: `tile` tokens, `at_once` of them at a time, each by heads_at_once x per_head threads.  Cosines and sines of the whole tile
+// are formed first; a thread then keeps those of its chunk in registers from head to head (read again from shared memory for each head, they took more of
+// the load/store unit than the numbers themselves).  Its first heads are requested before the cosines are formed.
+//   HALVES: item j < rotary / 2 / E holds numbers [E j, E j + E) and their partners rotary / 2 further on.  PAIRS: item j holds 2 E numbers side by
+//   side.  Items from there on copy E numbers (none where out is x).
+constexpr int ROPE_THREADS = 256;
+constexpr int ROPE_AHEAD = 4;            // heads of a thread that are requested together
+constexpr int ROPE_TURNS = 4;            // rounds of a CTA over its tokens
+struct RopeShape {
+    int32_t heads, rotary, per_head, heads_at_once, at_once, tile;
+    int64_t x_head, out_head;            // strides
+    double scale, sin_scale;
+    uint64_t zero = 0x8000000080000000ull;       // (-0, -0), as an argument: of a constant the compiler would make use
+};
+// `tokens`: how many there are; per_head <= ROPE_THREADS
+inline void rope_share(RopeShape &r, int64_t tokens, int sms)
+{
+    // a thread takes ROPE_AHEAD heads and a CTA ROPE_TURNS rounds, fewer where the tokens would not fill the GPU
+    int each = ROPE_AHEAD, turns = ROPE_TURNS;
+    auto threads = [&]() { return tokens * r.per_head * ((r.heads + each - 1) / each) / turns; };
+    while (turns > 1 && threads() < (int64_t)4 * sms * ROPE_THREADS) turns >>= 1;
+    while (each > 1 && threads() < (int64_t)2 * sms * ROPE_THREADS) each >>= 1;
+    r.heads_at_once = (r.heads + each - 1) / each;
+    if (r.heads_at_once * r.per_head > ROPE_THREADS) r.heads_at_once = ROPE_THREADS / r.per_head;
+    r.at_once = ROPE_THREADS / (r.heads_at_once * r.per_head);
+    if (tokens < r.at_once) r.at_once = (int)tokens;
+    r.tile = r.at_once * turns;
+    while (r.tile > r.at_once && r.tile * r.rotary > 8192) r.tile >>= 1;         // (at most 48 KB of cosines and sines)
+    if (r.tile < r.at_once) r.tile = r.at_once;
+}
+// floats of shared memory for a token's cosines and sines: chunks of E pairs are 16 bytes apart more than they are long, so that
+// neighbouring chunks' 16-byte reads meet no bank twice
+template <int E> __host__ __device__ constexpr int rope_cs_floats(int pairs) { return 2 * pairs + (E >= 4 ? 4 * (pairs / E) : 0); }
+
+// E numbers as they are stored
+template <typename T, int E> struct Raw {
+    uint4 v;
+    __device__ __forceinline__ void load(const T *p) { v = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<uint4 *>(p) = v; }
+    // numbers 2 i and 2 i + 1
+    __device__ __forceinline__ uint64_t pair(int i) const
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        if constexpr (sizeof(T) == 2) return sm100::pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+        else return sm100::pack2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    }
+    __device__ __forceinline__ void set(int i, uint64_t x)
+    {
+        float lo, hi;
+        sm100::unpack2(x, lo, hi);
+        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        if constexpr (sizeof(T) == 2) {
+            w[i] = sm100::pack_bf16x2(lo, hi);
+        } else {
+            w[2 * i] = __float_as_uint(lo);
+            w[2 * i + 1] = __float_as_uint(hi);
+        }
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <typename T> struct Raw<T, 1> {
+    float v;
+    __device__ __forceinline__ void load(const T *p) { v = load_as<float>(p, 0); }
+    __device__ __forceinline__ void store(T *p) const { store_from(p, 0, v); }
+};
+
+template <typename T, int E, bool HALVES, typename Token>
+__device__ __forceinline__ void rope_rows(const T *x, T *out, const RopeShape &r, const RopeTurns &turns, int64_t t0, int count, float *cs, Token token)
+{
+    const int pairs = r.rotary / 2, turn_items = pairs / E, row_cs = rope_cs_floats<E>(pairs);
+    const int per_token = r.heads_at_once * r.per_head;
+    const int t_first = threadIdx.x / per_token, rest = threadIdx.x - t_first * per_token, h0 = rest / r.per_head, j = rest - h0 * r.per_head;
+    const bool turn = j < turn_items;
+    const int o = turn ? (HALVES ? j * E : 2 * j * E) : r.rotary + (j - turn_items) * E, partner = HALVES ? pairs : E;
+    Raw<T, E> u[ROPE_AHEAD], w[ROPE_AHEAD];
+    int64_t from = 0, to = 0, pos = 0;
+    bool mine = t_first < r.at_once && t_first < count && token(t0 + t_first, from, to, pos);
+    auto request = [&](int first) {
+        const T *src = x + from + o + first * r.x_head;
+        const int64_t step = r.heads_at_once * r.x_head;
+#pragma unroll
+        for (int k = 0; k < ROPE_AHEAD; ++k) {
+            if (mine && first + k * r.heads_at_once < r.heads) {
+                u[k].load(src);
+                if (turn) w[k].load(src + partner);
+            }
+            src += step;
+        }
+    };
+    request(h0);
+    const uint64_t zero = r.zero;
+    for (int i = threadIdx.x; i < count * pairs; i += ROPE_THREADS) {
+        const int ti = i / pairs, p = i - ti * pairs;
+        int64_t f, g, at;
+        if (!token(t0 + ti, f, g, at)) continue;
+        const float2 c = rope_cos_sin(at, turns.turn[p], r.scale, r.sin_scale);
+        *reinterpret_cast<float2 *>(cs + ti * row_cs + 2 * p + (E >= 4 ? 4 * (p / E) : 0)) = c;
+    }
+    __syncthreads();
+    for (int t = t_first; t < count; t += r.at_once) {
+        if (t_first >= r.at_once) break;
+        if (t != t_first) {
+            mine = token(t0 + t, from, to, pos);
+            request(h0);
+        }
+        if (!mine) continue;
+        // HALVES: cosines and sines of pairs 2 i, 2 i + 1 side by side; PAIRS: (c, c) and (-s, s) of pair i
+        uint64_t cc[E > 1 ? E : 1], ss[E > 1 ? E : 1];
+        float2 one = make_float2(0.f, 0.f);
+        if (turn) {
+            const float *at = cs + t * row_cs + j * (2 * E + (E >= 4 ? 4 : 0));
+            if constexpr (E >= 2) {
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    const float4 v = *reinterpret_cast<const float4 *>(at + 2 * e);
+                    if constexpr (HALVES) {
+                        cc[e / 2] = sm100::pack2(v.x, v.z);
+                        ss[e / 2] = sm100::pack2(v.y, v.w);
+                    } else {
+                        cc[e] = sm100::pack2(v.x, v.x);
+                        ss[e] = sm100::pack2(-v.y, v.y);
+                        cc[e + 1] = sm100::pack2(v.z, v.z);
+                        ss[e + 1] = sm100::pack2(-v.w, v.w);
+                    }
+                }
+            } else {
+                one = *reinterpret_cast<const float2 *>(at);
+            }
+        }
+        for (int first = h0; first < r.heads; first += ROPE_AHEAD * r.heads_at_once) {
+            if (first != h0) request(first);
+            T *dst = out + to + o + first * r.out_head;
+            const int64_t step = r.heads_at_once * r.out_head;
+#pragma unroll
+            for (int k = 0; k < ROPE_AHEAD; ++k, dst += step) {
+                if (first + k * r.heads_at_once >= r.heads) continue;
+                if (turn) {
+                    // (-(b s) = b (-s): the products and sums of rope_turn, two at a time.  A product is written as an fma with -0, for a packed
+                    // product and sum are contracted to one fma whatever their rounding modes say)
+                    if constexpr (E == 1) {
+                        rope_turn(u[k].v, w[k].v, one);
+                    } else if constexpr (HALVES) {
+#pragma unroll
+                        for (int e = 0; e < E / 2; ++e) {
+                            const uint64_t a = u[k].pair(e), b = w[k].pair(e), ns = ss[e] ^ 0x8000000080000000ull;
+                            u[k].set(e, sm100::add2(sm100::fma2(a, cc[e], zero), sm100::fma2(b, ns, zero)));
+                            w[k].set(e, sm100::add2(sm100::fma2(b, cc[e], zero), sm100::fma2(a, ss[e], zero)));
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            Raw<T, E> &z = e < E / 2 ? u[k] : w[k];
+                            const uint64_t ab = z.pair(e % (E / 2));
+                            float a, b;
+                            sm100::unpack2(ab, a, b);
+                            z.set(e % (E / 2), sm100::add2(sm100::fma2(ab, cc[e], zero), sm100::fma2(sm100::pack2(b, a), ss[e], zero)));
+                        }
+                    }
+                    w[k].store(dst + partner);
+                }
+                u[k].store(dst);
+            }
+        }
+    }
+}
 
 }  // namespace elm
