@@ -100,35 +100,54 @@ __global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_const
                                 });
         return;
     }
-    // a token: 2 kv_heads rows of numbers (keys, values), G / 2 threads each
+    // items: (token, head, key or value, pair of groups); a thread requests its first one's numbers before the cosines are formed
     const int pairs = a.rotary / 2, row_cs = rope_cs_floats<16>(pairs);
     const int t0 = ((int)blockIdx.x - a.q_ctas) * a.tile;
-    const int count = min(a.tile, a.n_tokens - t0);
+    const int count = min(a.tile, a.n_tokens - t0), total = count * a.kv_heads * G;
+    int t, h, g0, g1, p;
+    bool key, halves, there;
+    uint32_t slot;
+    Raw<T, E> raw[2][C4_GROUP / E];
+    const int turned_key = a.rotary / C4_GROUP;                  // groups of a key that are rotated
+    auto request = [&](int i) {
+        const bool live = i < total;
+        const int j = i % G, th = live ? i / G : 0;
+        t = th / a.kv_heads;
+        h = th - t * a.kv_heads;
+        slot = (uint32_t)a.slots[t0 + t];
+        there = live && slot < a.n_slots;
+        key = j < HALF;
+        p = key ? j : j - HALF;
+        // the two groups: halves of pairs where they are rotated in halves, else side by side
+        halves = HALVES && key && 2 * p < turned_key;
+        g0 = halves ? p : 2 * p;
+        g1 = halves ? p + turned_key / 2 : 2 * p + 1;
+        if (there) {
+            const T *src = key ? (const T *)a.k + (int64_t)(t0 + t) * a.ks[0] + h * a.ks[1] : (const T *)a.v + (int64_t)(t0 + t) * a.vs[0] + h * a.vs[1];
+#pragma unroll
+            for (int e = 0; e < C4_GROUP / E; ++e) {
+                raw[0][e].load(src + g0 * C4_GROUP + e * E);
+                raw[1][e].load(src + g1 * C4_GROUP + e * E);
+            }
+        }
+    };
+    request(threadIdx.x);
     for (int i = threadIdx.x; i < count * pairs; i += APP_THREADS) {
-        const int t = i / pairs, p = i - t * pairs;
-        *reinterpret_cast<float2 *>(cs + t * row_cs + 2 * p + 4 * (p / 16)) = rope_cos_sin(a.positions[t0 + t], turns.turn[p], a.scale, a.scale);
+        const int ti = i / pairs, pi = i - ti * pairs;
+        *reinterpret_cast<float2 *>(cs + ti * row_cs + 2 * pi + 4 * (pi / 16)) = rope_cos_sin(a.positions[t0 + ti], turns.turn[pi], a.scale, a.scale);
     }
     __syncthreads();
-    const int total = count * a.kv_heads * G;                    // items: (token, head, key or value, pair of groups)
-    for (int i0 = threadIdx.x & ~31; i0 < total; i0 += APP_THREADS) {
-        const int i = i0 + (threadIdx.x & 31);
-        const bool live = i < total;
-        const int j = i % G, th = live ? i / G : 0, t = th / a.kv_heads, h = th - t * a.kv_heads;
-        const uint32_t slot = (uint32_t)a.slots[t0 + t];
-        const bool there = live && slot < a.n_slots;
-        const bool key = j < HALF;
-        const int p = key ? j : j - HALF;
-        // the two groups: halves of pairs while they are rotated in halves, else side by side
-        const int turned = key ? a.rotary / C4_GROUP : 0;        // groups that are rotated
-        const bool halves = HALVES && 2 * p < turned;
-        const int g0 = halves ? p : 2 * p, g1 = halves ? p + turned / 2 : 2 * p + 1;
+    for (int i0 = threadIdx.x & ~31; i0 < total; i0 += APP_THREADS) {        // (whole warps stay together: lanes exchange scales)
+        if (i0 >= APP_THREADS) request(i0 + (threadIdx.x & 31));
         uint32_t byte0 = 0, byte1 = 0;
         unsigned char *row = nullptr;
         if (there) {
-            const T *src = key ? (const T *)a.k + (int64_t)(t0 + t) * a.ks[0] + h * a.ks[1] : (const T *)a.v + (int64_t)(t0 + t) * a.vs[0] + h * a.vs[1];
             float x[C4_GROUP], y[C4_GROUP];
-            load_group<T, true>(src, g0 * C4_GROUP, x);
-            load_group<T, true>(src, g1 * C4_GROUP, y);
+#pragma unroll
+            for (int e = 0; e < C4_GROUP; e += 2) {
+                sm100::unpack2(raw[0][e / E].pair(e % E / 2), x[e], x[e + 1]);
+                sm100::unpack2(raw[1][e / E].pair(e % E / 2), y[e], y[e + 1]);
+            }
             if (halves) {
                 const float *c = cs + t * row_cs + p * 36;
 #pragma unroll
@@ -137,7 +156,7 @@ __global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_const
                     rope_turn(x[e], y[e], make_float2(v.x, v.y));
                     rope_turn(x[e + 1], y[e + 1], make_float2(v.z, v.w));
                 }
-            } else if (!HALVES && g0 < turned) {                 // (rotary is a multiple of 32: both groups or none)
+            } else if (!HALVES && key && g0 < turned_key) {      // (rotary is a multiple of 32: both groups or none)
                 const float *c = cs + t * row_cs + p * 36;
 #pragma unroll
                 for (int e = 0; e < C4_GROUP; e += 4) {
@@ -157,8 +176,8 @@ __global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_const
             codes[g0] = c0;
             codes[g1] = c1;
         }
-        // scales of the row's key or value: this thread's two, and its neighbours', as words
-        uint32_t w0 = 0, w1 = 0;                                 // scales of groups 0 .. 3 and 4 .. 7
+        // scales of the row's key or value, this thread's two and its neighbours', as words: of groups 0 .. 3 and 4 .. 7
+        uint32_t w0 = 0, w1 = 0;
         if (g0 < 4) w0 |= byte0 << (8 * g0);
         else w1 |= byte0 << (8 * (g0 - 4));
         if (g1 < 4) w0 |= byte1 << (8 * g1);
@@ -376,7 +395,7 @@ template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &t
         constexpr int E = 16 / (int)sizeof(T);
         int64_t q_ctas = 0;
         size_t smem = 0;
-        a.query = RopeShape{a.q_heads, a.rotary, 0, 0, 0, 0, a.qs[1], a.qos[1], a.scale, a.scale};
+        a.query = RopeShape{a.q_heads, a.rotary, 0, 0, 0, a.qs[1], a.qos[1], a.scale, a.scale};
         if (a.q_heads > 0) {
             // in place, numbers that are not rotated stay
             a.query.per_head = pairs / E + (a.q == a.q_out ? 0 : (D - a.rotary) / E);
@@ -386,7 +405,9 @@ template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &t
                 smem = (size_t)a.query.tile * rope_cs_floats<E>(pairs) * sizeof(float);
             }
         }
-        a.tile = tile_of(a.kv_heads * (D / C4_GROUP));
+        a.tile = APP_THREADS / (a.kv_heads * (D / C4_GROUP));   // an item a thread
+        if (a.tile > a.n_tokens / (2 * sms)) a.tile = a.n_tokens / (2 * sms);
+        if (a.tile < 1) a.tile = 1;
         const size_t rows_smem = (size_t)a.tile * rope_cs_floats<16>(pairs) * sizeof(float);
         if (rows_smem > smem) smem = rows_smem;
         const int64_t ctas = q_ctas + (a.n_tokens + a.tile - 1) / a.tile;

@@ -93,7 +93,7 @@ extern "C" int elm_rope(const void *X, const int32_t *positions, int64_t first_p
         a.xs[i] = xs[2 * i];
         a.os[i] = os[2 * i];
     }
-    a.shape = RopeShape{p->heads, p->rotary_dim, 0, 0, 0, 0, xs[1], os[1], p->scale, p->inverse ? -p->scale : p->scale};
+    a.shape = RopeShape{p->heads, p->rotary_dim, 0, 0, 0, xs[1], os[1], p->scale, p->inverse ? -p->scale : p->scale};
     a.n_tokens = p->n_tokens;
     a.tokens = (int64_t)p->batch * p->n_tokens;
     cudaStream_t st = (cudaStream_t)stream;

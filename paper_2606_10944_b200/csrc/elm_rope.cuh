@@ -95,16 +95,16 @@ template <typename T, int E> struct Chunk {
     }
 };
 
-// A CTA's share of a rotation: `tile` tokens, `at_once` of them at a time, each by heads_at_once x per_head threads.  Cosines and sines of the whole tile
-// are formed first; a thread then keeps those of its chunk in registers from head to head (read again from shared memory for each head, they took more of
-// the load/store unit than the numbers themselves).  Its first heads are requested before the cosines are formed.
+// A CTA's share of a rotation: `tile` tokens, each by heads_at_once x per_head threads.  Cosines and sines are formed first; a thread then keeps
+// those of its chunk in registers from head to head (read again from shared memory for each head, they took more of the load/store unit than the
+// numbers themselves).  Its first heads are requested before the cosines are formed; CTAs that go on to further tokens with the same cosine table
+// were slower (32 heads x 32768 tokens: 92 us; two rounds of tokens 104, four 112), for their loads then wait for their stores.
 //   HALVES: item j < rotary / 2 / E holds numbers [E j, E j + E) and their partners rotary / 2 further on.  PAIRS: item j holds 2 E numbers side by
 //   side.  Items from there on copy E numbers (none where out is x).
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_AHEAD = 4;            // heads of a thread that are requested together
-constexpr int ROPE_TURNS = 4;            // rounds of a CTA over its tokens
 struct RopeShape {
-    int32_t heads, rotary, per_head, heads_at_once, at_once, tile;
+    int32_t heads, rotary, per_head, heads_at_once, tile;
     int64_t x_head, out_head;            // strides
     double scale, sin_scale;
     uint64_t zero = 0x8000000080000000ull;       // (-0, -0), as an argument: of a constant the compiler would make use
@@ -112,18 +112,13 @@ struct RopeShape {
 // `tokens`: how many there are; per_head <= ROPE_THREADS
 inline void rope_share(RopeShape &r, int64_t tokens, int sms)
 {
-    // a thread takes ROPE_AHEAD heads and a CTA ROPE_TURNS rounds, fewer where the tokens would not fill the GPU
-    int each = ROPE_AHEAD, turns = ROPE_TURNS;
-    auto threads = [&]() { return tokens * r.per_head * ((r.heads + each - 1) / each) / turns; };
-    while (turns > 1 && threads() < (int64_t)4 * sms * ROPE_THREADS) turns >>= 1;
-    while (each > 1 && threads() < (int64_t)2 * sms * ROPE_THREADS) each >>= 1;
+    // a thread takes ROPE_AHEAD heads, fewer where the tokens would not fill the GPU
+    int each = ROPE_AHEAD;
+    while (each > 1 && tokens * r.per_head * ((r.heads + each - 1) / each) < (int64_t)2 * sms * ROPE_THREADS) each >>= 1;
     r.heads_at_once = (r.heads + each - 1) / each;
     if (r.heads_at_once * r.per_head > ROPE_THREADS) r.heads_at_once = ROPE_THREADS / r.per_head;
-    r.at_once = ROPE_THREADS / (r.heads_at_once * r.per_head);
-    if (tokens < r.at_once) r.at_once = (int)tokens;
-    r.tile = r.at_once * turns;
-    while (r.tile > r.at_once && r.tile * r.rotary > 8192) r.tile >>= 1;         // (at most 48 KB of cosines and sines)
-    if (r.tile < r.at_once) r.tile = r.at_once;
+    r.tile = ROPE_THREADS / (r.heads_at_once * r.per_head);
+    if (tokens < r.tile) r.tile = (int)tokens;
 }
 // floats of shared memory for a token's cosines and sines: chunks of E pairs are 16 bytes apart more than they are long, so that
 // neighbouring chunks' 16-byte reads meet no bank twice
@@ -166,12 +161,12 @@ __device__ __forceinline__ void rope_rows(const T *x, T *out, const RopeShape &r
 {
     const int pairs = r.rotary / 2, turn_items = pairs / E, row_cs = rope_cs_floats<E>(pairs);
     const int per_token = r.heads_at_once * r.per_head;
-    const int t_first = threadIdx.x / per_token, rest = threadIdx.x - t_first * per_token, h0 = rest / r.per_head, j = rest - h0 * r.per_head;
+    const int t = threadIdx.x / per_token, rest = threadIdx.x - t * per_token, h0 = rest / r.per_head, j = rest - h0 * r.per_head;
     const bool turn = j < turn_items;
     const int o = turn ? (HALVES ? j * E : 2 * j * E) : r.rotary + (j - turn_items) * E, partner = HALVES ? pairs : E;
     Raw<T, E> u[ROPE_AHEAD], w[ROPE_AHEAD];
     int64_t from = 0, to = 0, pos = 0;
-    bool mine = t_first < r.at_once && t_first < count && token(t0 + t_first, from, to, pos);
+    const bool mine = t < count && token(t0 + t, from, to, pos);
     auto request = [&](int first) {
         const T *src = x + from + o + first * r.x_head;
         const int64_t step = r.heads_at_once * r.x_head;
@@ -194,69 +189,62 @@ __device__ __forceinline__ void rope_rows(const T *x, T *out, const RopeShape &r
         *reinterpret_cast<float2 *>(cs + ti * row_cs + 2 * p + (E >= 4 ? 4 * (p / E) : 0)) = c;
     }
     __syncthreads();
-    for (int t = t_first; t < count; t += r.at_once) {
-        if (t_first >= r.at_once) break;
-        if (t != t_first) {
-            mine = token(t0 + t, from, to, pos);
-            request(h0);
-        }
-        if (!mine) continue;
-        // HALVES: cosines and sines of pairs 2 i, 2 i + 1 side by side; PAIRS: (c, c) and (-s, s) of pair i
-        uint64_t cc[E > 1 ? E : 1], ss[E > 1 ? E : 1];
-        float2 one = make_float2(0.f, 0.f);
-        if (turn) {
-            const float *at = cs + t * row_cs + j * (2 * E + (E >= 4 ? 4 : 0));
-            if constexpr (E >= 2) {
+    if (!mine) return;
+    // HALVES: cosines and sines of pairs 2 i, 2 i + 1 side by side; PAIRS: (c, c) and (-s, s) of pair i
+    uint64_t cc[E > 1 ? E : 1], ss[E > 1 ? E : 1];
+    float2 one = make_float2(0.f, 0.f);
+    if (turn) {
+        const float *at = cs + t * row_cs + j * (2 * E + (E >= 4 ? 4 : 0));
+        if constexpr (E >= 2) {
 #pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    const float4 v = *reinterpret_cast<const float4 *>(at + 2 * e);
-                    if constexpr (HALVES) {
-                        cc[e / 2] = sm100::pack2(v.x, v.z);
-                        ss[e / 2] = sm100::pack2(v.y, v.w);
-                    } else {
-                        cc[e] = sm100::pack2(v.x, v.x);
-                        ss[e] = sm100::pack2(-v.y, v.y);
-                        cc[e + 1] = sm100::pack2(v.z, v.z);
-                        ss[e + 1] = sm100::pack2(-v.w, v.w);
+            for (int e = 0; e < E; e += 2) {
+                const float4 v = *reinterpret_cast<const float4 *>(at + 2 * e);
+                if constexpr (HALVES) {
+                    cc[e / 2] = sm100::pack2(v.x, v.z);
+                    ss[e / 2] = sm100::pack2(v.y, v.w);
+                } else {
+                    cc[e] = sm100::pack2(v.x, v.x);
+                    ss[e] = sm100::pack2(-v.y, v.y);
+                    cc[e + 1] = sm100::pack2(v.z, v.z);
+                    ss[e + 1] = sm100::pack2(-v.w, v.w);
+                }
+            }
+        } else {
+            one = *reinterpret_cast<const float2 *>(at);
+        }
+    }
+    for (int first = h0; first < r.heads; first += ROPE_AHEAD * r.heads_at_once) {
+        if (first != h0) request(first);
+        T *dst = out + to + o + first * r.out_head;
+        const int64_t step = r.heads_at_once * r.out_head;
+#pragma unroll
+        for (int k = 0; k < ROPE_AHEAD; ++k, dst += step) {
+            if (first + k * r.heads_at_once >= r.heads) continue;
+            if (turn) {
+                // (-(b s) = b (-s): the products and sums of rope_turn, two at a time.  A product is written as an fma with -0, for a packed
+                // product and sum are contracted to one fma whatever their rounding modes say)
+                if constexpr (E == 1) {
+                    rope_turn(u[k].v, w[k].v, one);
+                } else if constexpr (HALVES) {
+#pragma unroll
+                    for (int e = 0; e < E / 2; ++e) {
+                        const uint64_t a = u[k].pair(e), b = w[k].pair(e), ns = ss[e] ^ 0x8000000080000000ull;
+                        u[k].set(e, sm100::add2(sm100::fma2(a, cc[e], zero), sm100::fma2(b, ns, zero)));
+                        w[k].set(e, sm100::add2(sm100::fma2(b, cc[e], zero), sm100::fma2(a, ss[e], zero)));
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        Raw<T, E> &z = e < E / 2 ? u[k] : w[k];
+                        const uint64_t ab = z.pair(e % (E / 2));
+                        float a, b;
+                        sm100::unpack2(ab, a, b);
+                        z.set(e % (E / 2), sm100::add2(sm100::fma2(ab, cc[e], zero), sm100::fma2(sm100::pack2(b, a), ss[e], zero)));
                     }
                 }
-            } else {
-                one = *reinterpret_cast<const float2 *>(at);
+                w[k].store(dst + partner);
             }
-        }
-        for (int first = h0; first < r.heads; first += ROPE_AHEAD * r.heads_at_once) {
-            if (first != h0) request(first);
-            T *dst = out + to + o + first * r.out_head;
-            const int64_t step = r.heads_at_once * r.out_head;
-#pragma unroll
-            for (int k = 0; k < ROPE_AHEAD; ++k, dst += step) {
-                if (first + k * r.heads_at_once >= r.heads) continue;
-                if (turn) {
-                    // (-(b s) = b (-s): the products and sums of rope_turn, two at a time.  A product is written as an fma with -0, for a packed
-                    // product and sum are contracted to one fma whatever their rounding modes say)
-                    if constexpr (E == 1) {
-                        rope_turn(u[k].v, w[k].v, one);
-                    } else if constexpr (HALVES) {
-#pragma unroll
-                        for (int e = 0; e < E / 2; ++e) {
-                            const uint64_t a = u[k].pair(e), b = w[k].pair(e), ns = ss[e] ^ 0x8000000080000000ull;
-                            u[k].set(e, sm100::add2(sm100::fma2(a, cc[e], zero), sm100::fma2(b, ns, zero)));
-                            w[k].set(e, sm100::add2(sm100::fma2(b, cc[e], zero), sm100::fma2(a, ss[e], zero)));
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            Raw<T, E> &z = e < E / 2 ? u[k] : w[k];
-                            const uint64_t ab = z.pair(e % (E / 2));
-                            float a, b;
-                            sm100::unpack2(ab, a, b);
-                            z.set(e % (E / 2), sm100::add2(sm100::fma2(ab, cc[e], zero), sm100::fma2(sm100::pack2(b, a), ss[e], zero)));
-                        }
-                    }
-                    w[k].store(dst + partner);
-                }
-                u[k].store(dst);
-            }
+            u[k].store(dst);
         }
     }
 }
