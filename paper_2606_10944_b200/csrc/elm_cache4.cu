@@ -9,7 +9,6 @@ namespace elm {
 namespace {
 
 constexpr int APP_THREADS = ROPE_THREADS;
-constexpr int APP_TILE = 32;             // tokens of a CTA at most (number by number)
 
 struct AppendArgs {
     const void *q, *k, *v;
@@ -43,8 +42,8 @@ __device__ __forceinline__ void load_group(const T *row, int first, float (&x)[C
     }
 }
 
-// HALVES with a group that lies in one half whose partners start on a 16-byte boundary (WIDE): the partners are loaded alike; any other
-// group number by number.  A partner is loaded by the other half's thread as well: from L1.
+// HALVES: WIDE means that halves are whole chunks of 16 bytes, so that the partners of a chunk are one as well; a partner is loaded by the other
+// half's thread, too: from L1.
 template <typename T, bool WIDE, bool HALVES>
 __device__ __forceinline__ void rotate_group(const T *row, int first, int rotary, const float2 *cs, float (&x)[C4_GROUP])
 {
@@ -54,30 +53,36 @@ __device__ __forceinline__ void rotate_group(const T *row, int first, int rotary
 #pragma unroll
         for (int i = 0; i < C4_GROUP; i += 2)
             if (first + i < rotary) rope_turn(x[i], x[i + 1], cs[(first + i) / 2]);
-    } else if (WIDE && half % C4_GROUP == 0) {
-        float y[C4_GROUP];
-        const bool lower = first < half;
-        load_group<T, true>(row, lower ? first + half : first - half, y);
-        const float2 *c = cs + (lower ? first : first - half);
-#pragma unroll
-        for (int i = 0; i < C4_GROUP; ++i) {
-            float a = lower ? x[i] : y[i], b = lower ? y[i] : x[i];
-            rope_turn(a, b, c[i]);
-            x[i] = lower ? a : b;
-        }
     } else {
+        constexpr int E = WIDE ? 16 / (int)sizeof(T) : 1;
 #pragma unroll
-        for (int i = 0; i < C4_GROUP; ++i) {
+        for (int i = 0; i < C4_GROUP; i += E) {
             const int j = first + i;
-            if (j < half) {
-                float b = load_as<float>(row, j + half);
-                rope_turn(x[i], b, cs[j]);
-            } else if (j < rotary) {
-                float a = load_as<float>(row, j - half);
-                rope_turn(a, x[i], cs[j - half]);
+            if (j >= rotary) continue;
+            const bool lower = j < half;
+            Chunk<T, E> other;
+            other.load(row + (lower ? j + half : j - half));
+            const float2 *c = cs + (lower ? j : j - half);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                float a = lower ? x[i + e] : other.v[e], b = lower ? other.v[e] : x[i + e];
+                rope_turn(a, b, c[e]);
+                x[i + e] = lower ? a : b;
             }
         }
     }
+}
+
+template <typename T, int E, bool HALVES> __device__ __forceinline__ void turn_queries(const AppendArgs &a, const RopeTurns &turns, float *cs)
+{
+    const int64_t t0 = (int64_t)blockIdx.x * a.query.tile;
+    rope_rows<T, E, HALVES>((const T *)a.q, (T *)a.q_out, a.query, turns, t0, min(a.query.tile, a.n_tokens - (int)t0), cs,
+                            [&](int64_t t, int64_t &from, int64_t &to, int64_t &pos) {
+                                from = t * a.qs[0];
+                                to = t * a.qos[0];
+                                pos = a.rotary ? a.positions[t] : 0;
+                                return (uint32_t)a.slots[t] < a.n_slots;
+                            });
 }
 
 // Queries are turned by the first CTAs as elm_rope does it; the others store rows, a thread two groups of 16 numbers: of a key that
@@ -90,14 +95,7 @@ __global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_const
     extern __shared__ __align__(16) float cs[];
     cudaGridDependencySynchronize();
     if ((int)blockIdx.x < a.q_ctas) {
-        const int64_t t0 = (int64_t)blockIdx.x * a.query.tile;
-        rope_rows<T, E, HALVES>((const T *)a.q, (T *)a.q_out, a.query, turns, t0, min(a.query.tile, a.n_tokens - (int)t0), cs,
-                                [&](int64_t t, int64_t &from, int64_t &to, int64_t &pos) {
-                                    from = t * a.qs[0];
-                                    to = t * a.qos[0];
-                                    pos = a.rotary ? a.positions[t] : 0;
-                                    return (uint32_t)a.slots[t] < a.n_slots;
-                                });
+        turn_queries<T, E, HALVES>(a, turns, cs);
         return;
     }
     // items: (token, head, key or value, pair of groups); a thread requests its first one's numbers before the cosines are formed
@@ -199,108 +197,50 @@ __global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_const
     }
 }
 
-// Rows whose numbers are not on 16-byte boundaries, or of which a part is rotated that does not end with a group: a thread takes a group of 16
-// numbers of a query, a key or a value.
+// Rows whose numbers are not on 16-byte boundaries, or of which a part is rotated that is not whole groups on both sides: a thread takes one group of
+// 16 numbers of a key or a value.  WIDE: on 16-byte boundaries, halves of the rotated part included.
 template <typename T, int D, bool WIDE, bool HALVES>
 __global__ void __launch_bounds__(APP_THREADS) append4_any_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTurns turns)
 {
     using R = Row4<D>;
     constexpr int G = R::GROUPS;
     extern __shared__ __align__(16) float cs_floats[];
-    float2 *cs = reinterpret_cast<float2 *>(cs_floats);        // [tile][rotary / 2]
     cudaGridDependencySynchronize();
+    if ((int)blockIdx.x < a.q_ctas) {
+        turn_queries<T, WIDE ? 16 / (int)sizeof(T) : 1, HALVES>(a, turns, cs_floats);
+        return;
+    }
+    float2 *cs = reinterpret_cast<float2 *>(cs_floats);        // [tile][rotary / 2]
     const int pairs = a.rotary / 2;
-    const int t0 = blockIdx.x * a.tile;
+    const int t0 = ((int)blockIdx.x - a.q_ctas) * a.tile;
     const int count = min(a.tile, a.n_tokens - t0);
     for (int i = threadIdx.x; i < count * pairs; i += APP_THREADS) {
         const int t = i / pairs;
         cs[i] = rope_cos_sin(a.positions[t0 + t], turns.turn[i - t * pairs], a.scale, a.scale);
     }
     __syncthreads();
-    const int per_token = (2 * a.kv_heads + a.q_heads) * G;
-    const int total = count * per_token;
-    // (whole warps stay together: the lanes of a row exchange their scales)
-    for (int i0 = threadIdx.x & ~31; i0 < total; i0 += APP_THREADS) {
+    const int total = count * a.kv_heads * 2 * G;
+    for (int i0 = threadIdx.x & ~31; i0 < total; i0 += APP_THREADS) {        // (whole warps stay together: lanes exchange scales)
         const int i = i0 + (threadIdx.x & 31);
         const bool live = i < total;
-        const int t = live ? i / per_token : 0, r = live ? i - t * per_token : 0;
+        const int j = i % (2 * G), th = live ? i / (2 * G) : 0;               // the row's group: keys, then values
+        const int t = th / a.kv_heads, h = th - t * a.kv_heads;
         const uint32_t slot = (uint32_t)a.slots[t0 + t];
-        const bool there = live && slot < a.n_slots;
-        const float2 *c = cs + t * pairs;
-        const int64_t tok = t0 + t;
-        const int kv_items = 2 * a.kv_heads * G;
         uint32_t byte = 0;
         unsigned char *row = nullptr;
-        int j = 0;
-        if (there && r < kv_items) {
-            const int h = r / (2 * G);
-            j = r - h * 2 * G;                                 // the row's group: keys, then values
+        if (live && slot < a.n_slots) {
+            const int64_t tok = t0 + t;
             const bool key = j < G;
             const T *src = key ? (const T *)a.k + tok * a.ks[0] + h * a.ks[1] : (const T *)a.v + tok * a.vs[0] + h * a.vs[1];
             const int first = (key ? j : j - G) * C4_GROUP;
             float x[C4_GROUP];
             load_group<T, WIDE>(src, first, x);
-            if (key) rotate_group<T, WIDE, HALVES>(src, first, a.rotary, c, x);
+            if (key) rotate_group<T, WIDE, HALVES>(src, first, a.rotary, cs + t * pairs, x);
             uint2 codes;
             byte = quantise4(x, codes);
             const uint32_t page = slot >> a.page_shift, in_page = slot & ((1u << a.page_shift) - 1u);
             row = a.rows + ((((uint64_t)page * (uint32_t)a.kv_heads + h) << a.page_shift) + in_page) * R::BYTES;
             *reinterpret_cast<uint2 *>(row + j * 8) = codes;
-        } else if (there) {
-            const int q = r - kv_items, h = q / G, first = (q - h * G) * C4_GROUP;
-            const T *src = (const T *)a.q + tok * a.qs[0] + h * a.qs[1];
-            T *dst = (T *)a.q_out + tok * a.qos[0] + h * a.qos[1];
-            if (HALVES && WIDE && a.rotary / 2 % C4_GROUP == 0) {
-                // a thread of the lower half takes both groups of its pairs, so that queries may be rotated in place
-                const int half = a.rotary / 2;
-                if (first < half || first >= a.rotary) {
-                    float x[C4_GROUP], y[C4_GROUP];
-                    const bool turn = first < half;
-                    load_group<T, true>(src, first, x);
-                    if (turn) {
-                        load_group<T, true>(src, first + half, y);
-#pragma unroll
-                        for (int e = 0; e < C4_GROUP; ++e) rope_turn(x[e], y[e], c[first + e]);
-                    }
-                    constexpr int E = 16 / (int)sizeof(T);
-#pragma unroll
-                    for (int e = 0; e < C4_GROUP; e += E) {
-                        Chunk<T, E> u, w;
-#pragma unroll
-                        for (int k = 0; k < E; ++k) {
-                            u.v[k] = x[e + k];
-                            if (turn) w.v[k] = y[e + k];
-                        }
-                        u.store(dst + first + e);
-                        if (turn) w.store(dst + first + half + e);
-                    }
-                }
-            } else if (HALVES) {
-                // pair by pair: this thread the pairs whose first number is in its group, and what is not rotated
-                const int half = a.rotary / 2;
-                for (int e = first; e < first + C4_GROUP; ++e) {
-                    if (e < half) {
-                        float x = load_as<float>(src, e), y = load_as<float>(src, e + half);
-                        rope_turn(x, y, c[e]);
-                        store_from(dst, e, x);
-                        store_from(dst, e + half, y);
-                    } else if (e >= a.rotary) {
-                        store_from(dst, e, load_as<float>(src, e));
-                    }
-                }
-            } else {
-                float x[C4_GROUP];
-                load_group<T, WIDE>(src, first, x);
-                rotate_group<T, WIDE, false>(src, first, a.rotary, c, x);
-                constexpr int E = WIDE ? 16 / (int)sizeof(T) : 1;
-#pragma unroll
-                for (int e = 0; e < C4_GROUP; e += E) {
-                    Chunk<T, E> u;
-#pragma unroll
-                    for (int k = 0; k < E; ++k) u.v[k] = x[e + k];
-                    u.store(dst + first + e);
-                }
-            }
         }
         // scales: a row's lanes are neighbours and start at a multiple of 4 lanes, so four of them fill a word
         uint32_t word = byte << (8 * (j & 3));
@@ -319,10 +259,11 @@ struct ReadArgs {
     void *k, *v;
     int32_t n;
     int64_t rows;                        // batch * kv_heads * n
+    int32_t each;                        // rows of a warp
 };
 
-// A warp takes 32 rows, whose places its lanes look up side by side, and makes one (d = 64: two) at a time: a lane 8 numbers, from 4 bytes of
-// codes, so that its stores are whole lines.
+// A warp takes up to 32 rows, whose places its lanes look up side by side, and makes one (d = 64: two) at a time: a lane 8 numbers, from 4
+// bytes of codes, so that its stores are whole lines.
 constexpr int READ_AHEAD = 8;            // rows (pairs of rows) requested together
 template <typename T, int D> __global__ void __launch_bounds__(256) read4_kernel(const __grid_constant__ ReadArgs a)
 {
@@ -330,10 +271,10 @@ template <typename T, int D> __global__ void __launch_bounds__(256) read4_kernel
     constexpr int AT_ONCE = 128 / D, LANES = 32 / AT_ONCE;       // rows of a step, lanes of a row
     cudaGridDependencySynchronize();
     const int lane = threadIdx.x & 31;
-    const int64_t first = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * 32;
+    const int64_t first = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * a.each;
     if (first >= a.rows) return;
     uint32_t place = NO_ROW;
-    if (first + lane < a.rows) {
+    if (lane < a.each && first + lane < a.rows) {
         const int64_t out_row = first + lane, problem = out_row / a.n, e = out_row - problem * a.n;
         const int b = (int)(problem / a.pool.kv_heads), h = (int)(problem - (int64_t)b * a.pool.kv_heads);
         const int64_t r = a.idx ? a.idx[out_row] : e;
@@ -342,9 +283,8 @@ template <typename T, int D> __global__ void __launch_bounds__(256) read4_kernel
     const int j = lane % LANES;
     const bool key = j < LANES / 2;
     T *out = (T *)(key ? a.k : a.v) + (j % (LANES / 2)) * 8;
-    const int64_t left = a.rows - first;
-#pragma unroll
-    for (int s0 = 0; s0 < 32 / AT_ONCE; s0 += READ_AHEAD) {
+    const int64_t left = min((int64_t)a.each, a.rows - first);
+    for (int s0 = 0; s0 * AT_ONCE < left; s0 += READ_AHEAD) {
         uint32_t codes[READ_AHEAD], scale[READ_AHEAD];
 #pragma unroll
         for (int s = 0; s < READ_AHEAD; ++s) {
@@ -381,48 +321,36 @@ template <typename T, int D> __global__ void __launch_bounds__(256) read4_kernel
     }
 }
 
-template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &turns, bool halves, bool wide, cudaStream_t st)
+template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &turns, bool halves, bool aligned, cudaStream_t st)
 {
-    const int sms = device_sm_count();
-    const int fill = a.n_tokens / (4 * sms);                     // tokens per CTA that would still fill the GPU
-    auto tile_of = [&](int per_token) {
-        int tile = (2 * APP_THREADS + per_token - 1) / per_token;
-        if (tile > fill) tile = fill < 1 ? 1 : fill;
-        return tile > APP_TILE ? APP_TILE : tile;
-    };
-    const int pairs = a.rotary / 2;
-    if (wide && a.rotary % 32 == 0) {
-        constexpr int E = 16 / (int)sizeof(T);
-        int64_t q_ctas = 0;
-        size_t smem = 0;
-        a.query = RopeShape{a.q_heads, a.rotary, 0, 0, 0, a.qs[1], a.qos[1], a.scale, a.scale};
-        if (a.q_heads > 0) {
-            // in place, numbers that are not rotated stay
-            a.query.per_head = pairs / E + (a.q == a.q_out ? 0 : (D - a.rotary) / E);
-            if (a.query.per_head > 0) {
-                rope_share(a.query, a.n_tokens, sms);
-                q_ctas = (a.n_tokens + a.query.tile - 1) / a.query.tile;
-                smem = (size_t)a.query.tile * rope_cs_floats<E>(pairs) * sizeof(float);
-            }
+    constexpr int E = 16 / (int)sizeof(T);
+    const int sms = device_sm_count(), pairs = a.rotary / 2;
+    const bool wide = aligned && pairs % E == 0, groups = wide && a.rotary % 32 == 0;
+    int64_t q_ctas = 0;
+    size_t smem = 0;
+    a.query = RopeShape{a.q_heads, a.rotary, 0, 0, 0, a.qs[1], a.qos[1], a.scale, a.scale};
+    if (a.q_heads > 0) {
+        const int e = wide ? E : 1;
+        a.query.per_head = pairs / e + (a.q == a.q_out ? 0 : (D - a.rotary) / e);       // (in place, numbers that are not rotated stay)
+        if (a.query.per_head > 0) {
+            rope_share(a.query, a.n_tokens, sms);
+            q_ctas = (a.n_tokens + a.query.tile - 1) / a.query.tile;
+            smem = (size_t)a.query.tile * (wide ? rope_cs_floats<E>(pairs) : rope_cs_floats<1>(pairs)) * sizeof(float);
         }
-        a.tile = APP_THREADS / (a.kv_heads * (D / C4_GROUP));   // an item a thread
-        if (a.tile > a.n_tokens / (2 * sms)) a.tile = a.n_tokens / (2 * sms);
-        if (a.tile < 1) a.tile = 1;
-        const size_t rows_smem = (size_t)a.tile * rope_cs_floats<16>(pairs) * sizeof(float);
-        if (rows_smem > smem) smem = rows_smem;
-        const int64_t ctas = q_ctas + (a.n_tokens + a.tile - 1) / a.tile;
-        if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
-        a.q_ctas = (int)q_ctas;
-        ELM_CUDA_TRY(launch_after(halves ? append4_kernel<T, D, true> : append4_kernel<T, D, false>, dim3((unsigned)ctas), dim3(APP_THREADS), smem, st, a, turns));
-        count_launches(1);
-        return cuda_status(cudaGetLastError());
     }
-    a.tile = tile_of((2 * a.kv_heads + a.q_heads) * (D / C4_GROUP));
-    const size_t smem = (size_t)a.tile * pairs * sizeof(float2);
-    const dim3 grid((unsigned)(((int64_t)a.n_tokens + a.tile - 1) / a.tile));
-    auto kern = wide ? (halves ? append4_any_kernel<T, D, true, true> : append4_any_kernel<T, D, true, false>)
-                     : (halves ? append4_any_kernel<T, D, false, true> : append4_any_kernel<T, D, false, false>);
-    ELM_CUDA_TRY(launch_after(kern, grid, dim3(APP_THREADS), smem, st, a, turns));
+    // an item a thread; fewer tokens per CTA where they would not fill the GPU
+    a.tile = APP_THREADS / (a.kv_heads * (D / C4_GROUP) * (groups ? 1 : 2));
+    if (a.tile > a.n_tokens / (2 * sms)) a.tile = a.n_tokens / (2 * sms);
+    if (a.tile < 1) a.tile = 1;
+    const size_t rows_smem = (size_t)a.tile * (groups ? rope_cs_floats<16>(pairs) : 2 * pairs) * sizeof(float);
+    if (rows_smem > smem) smem = rows_smem;
+    const int64_t ctas = q_ctas + (a.n_tokens + a.tile - 1) / a.tile;
+    if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
+    a.q_ctas = (int)q_ctas;
+    auto kern = groups ? (halves ? append4_kernel<T, D, true> : append4_kernel<T, D, false>)
+                : wide ? (halves ? append4_any_kernel<T, D, true, true> : append4_any_kernel<T, D, true, false>)
+                       : (halves ? append4_any_kernel<T, D, false, true> : append4_any_kernel<T, D, false, false>);
+    ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)ctas), dim3(APP_THREADS), smem, st, a, turns));
     count_launches(1);
     return cuda_status(cudaGetLastError());
 }
@@ -514,7 +442,10 @@ extern "C" int elm_cache4_read(const void *rows, const int32_t *table, const int
     a.v = V_out;
     a.n = p->n_kv;
     a.rows = (int64_t)p->batch * p->kv_heads * p->n_kv;
-    const int64_t ctas = (a.rows + 255) / 256;
+    // rows of a warp: 32 in long calls (they are looked up side by side), fewer where the warps would not fill the GPU
+    a.each = 32;
+    while (a.each > 8 && a.rows / a.each < (int64_t)32 * device_sm_count()) a.each >>= 1;
+    const int64_t ctas = (a.rows + 8 * a.each - 1) / (8 * a.each);
     if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
     auto kern = p->dtype == ELM_BF16 ? (p->d == 64 ? read4_kernel<__nv_bfloat16, 64> : read4_kernel<__nv_bfloat16, 128>)
                                      : (p->d == 64 ? read4_kernel<float, 64> : read4_kernel<float, 128>);
