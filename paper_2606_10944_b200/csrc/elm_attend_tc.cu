@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(256) gather4_tc_kernel(Pool4 pool, const int32
                 const unsigned char *from = pool.rows + (uint64_t)row * R::BYTES;
                 const int j = (lane >> 4) * (D / 8) + chunk;
                 codes8_to_half2(*reinterpret_cast<const uint32_t *>(from + 4 * j), x);
-                const uint32_t s = scale4_half_bits(from[R::SCALES + j / 2]) * 0x10001u;
+                const uint32_t s = scale4_half2(from[R::SCALES + j / 2]);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const uint32_t y = hmul2_bits(x[k], s);

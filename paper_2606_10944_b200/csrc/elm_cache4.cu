@@ -301,7 +301,7 @@ template <typename T, int D> __global__ void __launch_bounds__(256) read4_kernel
             const int at = (s0 + s) * AT_ONCE + lane / LANES;
             uint32_t half2s[4];
             codes8_to_half2(codes[s], half2s);
-            const uint32_t sc = scale4_half_bits(scale[s]) * 0x10001u;
+            const uint32_t sc = scale4_half2(scale[s]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) half2s[k] = hmul2_bits(half2s[k], sc);
             if (at >= left) continue;

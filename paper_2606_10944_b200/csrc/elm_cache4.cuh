@@ -53,6 +53,9 @@ inline bool pool_fits(int n_pages, int page_rows, int kv_heads)
 
 // the scale's byte as fp16: sign left out, 5 exponent and 3 mantissa bits in the places of an fp16 number's upper ones
 __device__ __forceinline__ uint32_t scale4_half_bits(uint32_t byte) { return byte << 7; }
+// two of them side by side (products: the units that shift and convert have more to do than those that multiply)
+__device__ __forceinline__ uint32_t scale4_half2(uint32_t low, uint32_t high) { return low * 0x80u + high * 0x800000u; }
+__device__ __forceinline__ uint32_t scale4_half2(uint32_t both) { return both * 0x00800080u; }
 
 // Two codes (a byte, the lower half first) as two fp16 numbers.  Codes are at most 6, scales at most 10240 with 4 bits, products have 6
 // bits and are at most 61440: fp16 holds them exactly, and so does bf16.

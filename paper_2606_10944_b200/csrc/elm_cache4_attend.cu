@@ -87,6 +87,13 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// the same without sums from before
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
 {
     uint32_t y;
@@ -185,7 +192,7 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
     constexpr int N = C::N, KS = C::KS;
     constexpr int KB = D / 8, VB = D / 16;                       // bytes of codes a lane reads of a key row, of a value row
     extern __shared__ __align__(16) unsigned char smem[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     float *ml = reinterpret_cast<float *>(smem + C::OFF_ML);
     float *q_scale = reinterpret_cast<float *>(smem + C::OFF_QS);
     uint4 *q_frag = reinterpret_cast<uint4 *>(smem + C::OFF_Q);
@@ -259,11 +266,10 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                     if (next_row[0] != NO_ROW) next_bias = log2f(w);
                 }
             } else {
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int e = tile * A4_TILE + 16 * x;
-                    if (e < rq.rows) next_row[x] = pool_row(a.pool, b, h, e);
-                }
+                const int e = tile * A4_TILE;                    // (below the rows that are seen)
+                next_row[0] = pool_row(a.pool, b, h, e);
+                if (a.pool.page_shift > 4) next_row[1] = next_row[0] == NO_ROW ? NO_ROW : next_row[0] + 16;
+                else if (e + 16 < rq.rows) next_row[1] = pool_row(a.pool, b, h, e + 16);
             }
         };
         uint32_t gone = 0;                                       // two bits per stage: halves that are on no page
@@ -282,16 +288,17 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                 } else {
                     const bool there0 = next_row[0] != NO_ROW, there1 = next_row[1] != NO_ROW;
                     gone = (gone & ~(3u << (2 * stage))) | ((there0 ? 0u : 1u) << (2 * stage)) | ((there1 ? 0u : 2u) << (2 * stage));
-                    const unsigned char *p0 = a.pool.rows + (there0 ? (uint64_t)next_row[0] * R::BYTES + lane * 16 : 0);
-                    // (the second half begins with chunk 16 CHUNKS, in the middle of the middle round)
-                    const unsigned char *p1 = a.pool.rows + (there1 ? (uint64_t)next_row[1] * R::BYTES + lane * 16 : 0);
+                    // (nothing is read for a half that is not there)
+                    const unsigned char *p0 = a.pool.rows + (there0 ? (uint64_t)next_row[0] * R::BYTES : 0) + lane * 16;
+                    // the second half begins with chunk 16 CHUNKS, in the middle of the middle round
                     constexpr int MID = R::CHUNKS / 2;
-#pragma unroll
-                    for (int i = 0; i < MID; ++i) cp16(dst + i * 512, p0 + (there0 ? i * 512 : 0), there0);
+                    const unsigned char *p1 = a.pool.rows + (there1 ? (uint64_t)next_row[1] * R::BYTES : 0) + lane * 16;
                     const bool up = lane >= 16;
-                    cp16(dst + MID * 512, up ? p1 - (there1 ? 256 : 0) : p0 + (there0 ? MID * 512 : 0), up ? there1 : there0);
 #pragma unroll
-                    for (int i = MID + 1; i < R::CHUNKS; ++i) cp16(dst + i * 512, p1 + (there1 ? i * 512 - MID * 512 - 256 : 0), there1);
+                    for (int i = 0; i < MID; ++i) cp16(dst + i * 512, p0 + i * 512, there0);
+                    cp16(dst + MID * 512, up ? p1 - 256 : p0 + MID * 512, up ? there1 : there0);
+#pragma unroll
+                    for (int i = MID + 1; i < R::CHUNKS; ++i) cp16(dst + i * 512, p1 + (i * 512 - MID * 512 - 256), there1);
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
@@ -401,54 +408,55 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
 
             // ---- logits: s[block of 16 rows][tile of vectors] = rows g, g + 8 x vectors 2t, 2t + 1 ----
             float s[2][NT][4];
+            uint32_t codes[2][2][KB / 4], scale[2][2][D / 64];
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                uint32_t codes[2][KB / 4], scale[2];
+            for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const unsigned char *row = rows + (kb * 16 + x * 8 + g) * R::BYTES;
                     if constexpr (D == 128) {
                         const uint4 c = *reinterpret_cast<const uint4 *>(row + t * KB);
-                        codes[x][0] = c.x; codes[x][1] = c.y; codes[x][2] = c.z; codes[x][3] = c.w;
-                        scale[x] = *reinterpret_cast<const unsigned short *>(row + R::SCALES + 2 * t);
+                        codes[kb][x][0] = c.x; codes[kb][x][1] = c.y; codes[kb][x][2] = c.z; codes[kb][x][3] = c.w;
                     } else {
                         const uint2 c = *reinterpret_cast<const uint2 *>(row + t * KB);
-                        codes[x][0] = c.x; codes[x][1] = c.y;
-                        scale[x] = row[R::SCALES + t];
+                        codes[kb][x][0] = c.x; codes[kb][x][1] = c.y;
                     }
+#pragma unroll
+                    for (int y = 0; y < D / 64; ++y) scale[kb][x][y] = scale4_half2(row[R::SCALES + D / 64 * t + y]);
                 }
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+            for (int w = 0; w < KB / 4; ++w) {                   // a word: eight numbers, two steps
+                uint4 q[PARTS][NT];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) s[kb][n][x] = 0.f;
+                for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-                for (int w = 0; w < KB / 4; ++w) {               // a word: eight numbers, two steps
+                    for (int n = 0; n < NT; ++n) q[p][n] = q_frag[((p * NT + n) * (KS / 2) + w) * 32 + lane];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
                     uint32_t half[2][4];
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        codes8_to_half2(codes[x][w], half[x]);
-                        const uint32_t sc = scale4_half_bits(D == 128 && w >= 2 ? scale[x] >> 8 : scale[x] & 0xffu) * 0x10001u;
+                        codes8_to_half2(codes[kb][x][w], half[x]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) half[x][i] = hmul2_bits(half[x][i], sc);
+                        for (int i = 0; i < 4; ++i) half[x][i] = hmul2_bits(half[x][i], scale[kb][x][w / 2]);
                     }
                     const uint32_t a0[4] = {half[0][0], half[1][0], half[0][1], half[1][1]};
                     const uint32_t a1[4] = {half[0][2], half[1][2], half[0][3], half[1][3]};
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         if constexpr (PARTS == 1) {
-                            const uint4 q = q_frag[(n * (KS / 2) + w) * 32 + lane];
-                            mma_f16(s[kb][n], a0, q.x, q.y);
-                            mma_f16(s[kb][n], a1, q.z, q.w);
+                            if (w == 0) mma_f16_first(s[kb][n], a0, q[0][n].x, q[0][n].y);
+                            else mma_f16(s[kb][n], a0, q[0][n].x, q[0][n].y);
+                            mma_f16(s[kb][n], a1, q[0][n].z, q[0][n].w);
                         } else {
                             // a chain of four, the small parts first
-                            float c[4] = {0.f, 0.f, 0.f, 0.f};
-                            const uint4 lo = q_frag[((NT + n) * (KS / 2) + w) * 32 + lane], hi = q_frag[(n * (KS / 2) + w) * 32 + lane];
-                            mma_f16(c, a0, lo.x, lo.y);
-                            mma_f16(c, a1, lo.z, lo.w);
-                            mma_f16(c, a0, hi.x, hi.y);
-                            mma_f16(c, a1, hi.z, hi.w);
+                            float c[4];
+                            mma_f16_first(c, a0, q[1][n].x, q[1][n].y);
+                            mma_f16(c, a1, q[1][n].z, q[1][n].w);
+                            mma_f16(c, a0, q[0][n].x, q[0][n].y);
+                            mma_f16(c, a1, q[0][n].z, q[0][n].w);
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) s[kb][n][x] += c[x];
+                            for (int x = 0; x < 4; ++x) s[kb][n][x] = w == 0 ? c[x] : s[kb][n][x] + c[x];
                         }
                     }
                 }
@@ -493,20 +501,20 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) top[n][y] = fmaxf(top[n][y], fmaxf(s[kb][n][y], s[kb][n][2 + y]));
+            // The reference moves when some row has passed it by A4_SLACK (the first rows seen do: it is -inf); only then the lanes that hold a
+            // vector's rows ask one another for the largest.
             bool moved = false;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-#pragma unroll
-                    for (int off = 4; off < 32; off <<= 1) top[n][y] = fmaxf(top[n][y], __shfl_xor_sync(0xffffffffu, top[n][y], off));
-                    moved |= top[n][y] > ref[n][y] + A4_SLACK;   // (the first rows seen, too: ref is -inf)
-                }
+                for (int y = 0; y < 2; ++y) moved |= top[n][y] > ref[n][y] + A4_SLACK;
             if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) top[n][y] = fmaxf(top[n][y], __shfl_xor_sync(0xffffffffu, top[n][y], off));
                         const float to = fmaxf(ref[n][y], top[n][y]);
                         const float f2 = ref[n][y] == -INFINITY ? 0.f : exp2_fast(ref[n][y] - to);
                         ref[n][y] = to;
@@ -553,7 +561,7 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                         }
                     }
                     const int sg = R::SCALES + R::GROUPS + (D == 128 ? g : g / 2);
-                    vs[kb][x] = scale4_half_bits(row[sg]) | (scale4_half_bits(row[R::BYTES + sg]) << 16);
+                    vs[kb][x] = scale4_half2(row[sg], row[R::BYTES + sg]);
                 }
 #pragma unroll
             for (int w = 0; w < VB / 4; ++w) {
@@ -582,8 +590,8 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                             mma_f16(acc, a0, pb[0][0][n][0], pb[0][0][n][1]);
                             mma_f16(acc, a1, pb[0][1][n][0], pb[0][1][n][1]);
                         } else {
-                            float c[4] = {0.f, 0.f, 0.f, 0.f};
-                            mma_f16(c, a0, pb[1][0][n][0], pb[1][0][n][1]);
+                            float c[4];
+                            mma_f16_first(c, a0, pb[1][0][n][0], pb[1][0][n][1]);
                             mma_f16(c, a1, pb[1][1][n][0], pb[1][1][n][1]);
                             mma_f16(c, a0, pb[0][0][n][0], pb[0][0][n][1]);
                             mma_f16(c, a1, pb[0][1][n][0], pb[0][1][n][1]);
