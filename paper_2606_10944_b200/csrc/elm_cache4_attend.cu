@@ -26,6 +26,7 @@
 
 #include "elm_attend.cuh"
 #include "elm_cache4.cuh"
+#include "elm_sm100.cuh"
 
 namespace elm {
 namespace {
@@ -185,7 +186,7 @@ __device__ __forceinline__ int request_of(const int64_t *prefix, int batch, int6
 
 // LIST: entries idx with weights w, looked up row by row; else a request's rows, in pages of at least 16: half a tile lies in one page.
 template <typename T, int D, int NT, int PARTS, bool LIST>
-__global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(const __grid_constant__ Attend4Args a)
+__global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) attend4_kernel(const __grid_constant__ Attend4Args a)
 {
     using C = A4<D, NT, PARTS>;
     using R = Row4<D>;
@@ -253,11 +254,13 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
         // ---- the rows of this warp's tiles, looked up a tile before they are fetched ----
         uint32_t next_row[2] = {NO_ROW, NO_ROW};                 // LIST: [0] is lane's row of the tile; else the first rows of its halves
         float next_bias = -INFINITY;
+        const int share = (tile_end - tile0 + A4_WARPS - 1) / A4_WARPS, mine0 = tile0 + warp * share, mine1 = min(mine0 + share, tile_end);
+        const int page_mask = (1 << a.pool.page_shift) - 1;
         auto look_up = [&](int tile) {
-            next_row[0] = next_row[1] = NO_ROW;
-            next_bias = -INFINITY;
-            if (tile >= tile_end) return;
+            if (tile >= mine1) return;
             if constexpr (LIST) {
+                next_row[0] = NO_ROW;
+                next_bias = -INFINITY;
                 const int e = tile * A4_TILE + lane;
                 if (e < rq.rows) {
                     const int64_t at = ((int64_t)b * a.pool.kv_heads + h) * a.n_kv + e;
@@ -267,13 +270,18 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                 }
             } else {
                 const int e = tile * A4_TILE;                    // (below the rows that are seen)
-                next_row[0] = pool_row(a.pool, b, h, e);
-                if (a.pool.page_shift > 4) next_row[1] = next_row[0] == NO_ROW ? NO_ROW : next_row[0] + 16;
-                else if (e + 16 < rq.rows) next_row[1] = pool_row(a.pool, b, h, e + 16);
+                if (a.pool.page_shift == 4) {
+                    next_row[0] = pool_row(a.pool, b, h, e);
+                    next_row[1] = e + 16 < rq.rows ? pool_row(a.pool, b, h, e + 16) : NO_ROW;
+                } else if (tile == mine0 || (e & page_mask) == 0) {
+                    next_row[0] = pool_row(a.pool, b, h, e);
+                } else if (next_row[0] != NO_ROW) {
+                    next_row[0] += A4_TILE;                      // (the same page)
+                }
             }
         };
-        uint32_t gone = 0;                                       // two bits per stage: halves that are on no page
-        auto fetch = [&](int stage, bool any) {
+        uint32_t gone = 0;                                       // two bits for each tile in flight: halves that are on no page
+        auto fetch = [&](int stage, bool any, int order) {
             if (any) {
                 const uint32_t dst = ring_u32 + stage * C::TILE_BYTES + lane * 16;
                 if constexpr (LIST) {
@@ -286,30 +294,35 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                         cp16(dst + i * 512, a.pool.rows + (from != NO_ROW ? (uint64_t)from * R::BYTES + chunk * 16 : 0), from != NO_ROW);
                     }
                 } else {
-                    const bool there0 = next_row[0] != NO_ROW, there1 = next_row[1] != NO_ROW;
-                    gone = (gone & ~(3u << (2 * stage))) | ((there0 ? 0u : 1u) << (2 * stage)) | ((there1 ? 0u : 2u) << (2 * stage));
-                    // (nothing is read for a half that is not there)
+                    // (nothing is read for what is not there)
+                    const bool there0 = next_row[0] != NO_ROW;
                     const unsigned char *p0 = a.pool.rows + (there0 ? (uint64_t)next_row[0] * R::BYTES : 0) + lane * 16;
-                    // the second half begins with chunk 16 CHUNKS, in the middle of the middle round
-                    constexpr int MID = R::CHUNKS / 2;
-                    const unsigned char *p1 = a.pool.rows + (there1 ? (uint64_t)next_row[1] * R::BYTES : 0) + lane * 16;
-                    const bool up = lane >= 16;
+                    if (a.pool.page_shift > 4) {
 #pragma unroll
-                    for (int i = 0; i < MID; ++i) cp16(dst + i * 512, p0 + i * 512, there0);
-                    cp16(dst + MID * 512, up ? p1 - 256 : p0 + MID * 512, up ? there1 : there0);
+                        for (int i = 0; i < R::CHUNKS; ++i) cp16(dst + i * 512, p0 + i * 512, there0);
+                        if (!there0) gone |= 3u << (2 * order);
+                    } else {
+                        // the second half begins with chunk 16 CHUNKS, in the middle of the middle round
+                        constexpr int MID = R::CHUNKS / 2;
+                        const bool there1 = next_row[1] != NO_ROW, up = lane >= 16;
+                        const unsigned char *p1 = a.pool.rows + (there1 ? (uint64_t)next_row[1] * R::BYTES : 0) + lane * 16;
 #pragma unroll
-                    for (int i = MID + 1; i < R::CHUNKS; ++i) cp16(dst + i * 512, p1 + (i * 512 - MID * 512 - 256), there1);
+                        for (int i = 0; i < MID; ++i) cp16(dst + i * 512, p0 + i * 512, there0);
+                        cp16(dst + MID * 512, up ? p1 - 256 : p0 + MID * 512, up ? there1 : there0);
+#pragma unroll
+                        for (int i = MID + 1; i < R::CHUNKS; ++i) cp16(dst + i * 512, p1 + (i * 512 - MID * 512 - 256), there1);
+                        gone |= ((there0 ? 0u : 1u) | (there1 ? 0u : 2u)) << (2 * order);
+                    }
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        int ahead = tile0 + warp;
+        int ahead = mine0;
         look_up(ahead);
 #pragma unroll
         for (int s = 0; s < A4_STAGES - 1; ++s) {
-            fetch(s, ahead < tile_end);
-            ahead += A4_WARPS;
-            look_up(ahead);
+            fetch(s, ahead < mine1, s);
+            look_up(++ahead);
         }
 
         // ---- queries: vector v by the threads of a 16th of the CTA; scaled by a power of two, laid out as the lanes want them ----
@@ -355,6 +368,7 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
 
         // ---- the warp's tiles ----
         float o[NT][KS][4], l[NT][2], ref[NT][2], qs[NT][2];
+        float limit[NT][2], lift[NT][2];                         // what moves the reference; what a logit is raised by
         int seen[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -362,7 +376,8 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
             for (int x = 0; x < 2; ++x) {
                 const int v = n * 8 + 2 * t + x;
                 l[n][x] = 0.f;
-                ref[n][x] = -INFINITY;
+                ref[n][x] = limit[n][x] = -INFINITY;
+                lift[n][x] = 0.f;
                 qs[n][x] = q_scale[v];
                 seen[n][x] = tail ? rq.rows - rq.tokens + 1 + (vec0 + v) / a.rep : rq.rows;
             }
@@ -372,26 +387,26 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                 for (int x = 0; x < 4; ++x) o[n][i][x] = 0.f;
         }
         int stage = 0;
-        for (int tile = tile0 + warp; tile < tile_end; tile += A4_WARPS) {
+        const int cut_tile = first_seen / A4_TILE;               // from this one on some vector does not see all rows
+        for (int tile = mine0; tile < mine1; ++tile) {
             asm volatile("cp.async.wait_group %0;" ::"n"(A4_STAGES - 2) : "memory");
             __syncwarp();
             const unsigned char *rows = ring + stage * C::TILE_BYTES;
             const float *rb = bias + stage * A4_TILE;
-            const uint32_t gone_of = (gone >> (2 * stage)) & 3u;
+            const uint32_t gone_now = gone & 3u;
+            gone >>= 2;
             {
                 // the stage read in the last round is free
                 const int to = stage + A4_STAGES - 1;
-                fetch(to >= A4_STAGES ? to - A4_STAGES : to, ahead < tile_end);
-                ahead += A4_WARPS;
-                look_up(ahead);
+                fetch(to >= A4_STAGES ? to - A4_STAGES : to, ahead < mine1, A4_STAGES - 2);
+                look_up(++ahead);
             }
             stage = stage + 1 == A4_STAGES ? 0 : stage + 1;
 
-            const bool cut = (tile + 1) * A4_TILE > first_seen;
+            const bool cut = tile >= cut_tile;
             // a value that is NaN must not reach a vector that does not see its row through 0 x NaN: such scales are taken out here and put
             // back as NaN sums of those that see it
             uint32_t nan_groups = 0, nan_rows = 0;
-            const uint32_t gone_now = LIST ? 0u : gone_of;
             if (!LIST && cut) {
                 // rows behind the last one came with their page, whatever they hold: nothing
                 if (tile * A4_TILE + lane >= rq.rows) *reinterpret_cast<uint4 *>(ring + (rows - ring) + lane * R::BYTES + R::SCALES) = make_uint4(0u, 0u, 0u, 0u);
@@ -462,10 +477,8 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                 }
             }
 
-            // ---- logits in base 2 with the weights; what is not seen is -inf whatever it holds ----
+            // ---- what is not seen is -inf whatever it holds; LIST: logits in base 2 with the weights, else as they are (times qs: base 2) ----
             float top[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY;
             if (!LIST && (cut || gone_now)) {
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
@@ -475,39 +488,36 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
-                            for (int y = 0; y < 2; ++y) {
-                                const bool out = at >= seen[n][y] || ((gone_now >> kb) & 1u);
-                                s[kb][n][2 * x + y] = out ? -INFINITY : s[kb][n][2 * x + y] * qs[n][y];
-                            }
+                            for (int y = 0; y < 2; ++y)
+                                if (at >= seen[n][y] || ((gone_now >> kb) & 1u)) s[kb][n][2 * x + y] = -INFINITY;
                     }
-            } else {
+            }
+            if constexpr (LIST) {
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const float lw = LIST ? rb[kb * 16 + x * 8 + g] : 0.f;
+                        const float lw = rb[kb * 16 + x * 8 + g];
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
-                            for (int y = 0; y < 2; ++y) {
-                                float &z = s[kb][n][2 * x + y];
-                                z = LIST ? fmaf(z, qs[n][y], lw) : z * qs[n][y];
-                            }
+                            for (int y = 0; y < 2; ++y) s[kb][n][2 * x + y] = fmaf(s[kb][n][2 * x + y], qs[n][y], lw);
                     }
             }
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) top[n][y] = fmaxf(top[n][y], fmaxf(s[kb][n][y], s[kb][n][2 + y]));
+                for (int y = 0; y < 2; ++y) {
+                    top[n][y] = fmaxf(sm100::max3(s[0][n][y], s[0][n][2 + y], s[1][n][y]), s[1][n][2 + y]);
+                    if (!LIST) top[n][y] *= qs[n][y];
+                }
             // The reference moves when some row has passed it by A4_SLACK (the first rows seen do: it is -inf); only then the lanes that hold a
             // vector's rows ask one another for the largest.
             bool moved = false;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) moved |= top[n][y] > ref[n][y] + A4_SLACK;
+                for (int y = 0; y < 2; ++y) moved |= top[n][y] > limit[n][y];
             if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -518,6 +528,8 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
                         const float to = fmaxf(ref[n][y], top[n][y]);
                         const float f2 = ref[n][y] == -INFINITY ? 0.f : exp2_fast(ref[n][y] - to);
                         ref[n][y] = to;
+                        limit[n][y] = to + A4_SLACK;
+                        lift[n][y] = to == -INFINITY ? 0.f : A4_LIFT - to;
                         l[n][y] *= f2;
 #pragma unroll
                         for (int i = 0; i < KS; ++i) {
@@ -530,12 +542,12 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
             uint32_t pb[PARTS][2][NT][2];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float r0 = ref[n][0] == -INFINITY ? 0.f : ref[n][0] - A4_LIFT, r1 = ref[n][1] == -INFINITY ? 0.f : ref[n][1] - A4_LIFT;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const float p0 = exp2_fast(s[kb][n][2 * x] - r0), p1 = exp2_fast(s[kb][n][2 * x + 1] - r1);
+                        const float p0 = exp2_fast(LIST ? s[kb][n][2 * x] + lift[n][0] : fmaf(s[kb][n][2 * x], qs[n][0], lift[n][0]));
+                        const float p1 = exp2_fast(LIST ? s[kb][n][2 * x + 1] + lift[n][1] : fmaf(s[kb][n][2 * x + 1], qs[n][1], lift[n][1]));
                         l[n][0] += p0;
                         l[n][1] += p1;
                         const uint32_t hi = half2_bits(p0, p1);
@@ -571,7 +583,7 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 4 : 3) attend4_kernel(co
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         const uint32_t r0 = vw[kb][x][0][w], r1 = vw[kb][x][1][w];
-                        codes8_to_half2((r0 & 0x0f0f0f0fu) | ((r1 << 4) & 0xf0f0f0f0u), even[kb][x]);
+                        codes8_to_half2((r0 & 0x0f0f0f0fu) | ((r1 * 16u) & 0xf0f0f0f0u), even[kb][x]);
                         codes8_to_half2(((r0 >> 4) & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u), odd[kb][x]);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
