@@ -35,7 +35,7 @@ constexpr int A4_WARPS = 4;
 constexpr int A4_THREADS = 32 * A4_WARPS;
 constexpr int A4_TILE = 32;              // rows of a warp's tile
 constexpr int A4_STAGES = 2;
-constexpr int A4_START = 12;              // what a problem's beginning and end cost, in tiles
+constexpr int A4_START = 16;              // what a problem's beginning and end cost, in tiles
 constexpr int A4_MAX_BATCH = 1024, A4_FEW = 127;                // requests of a call; of one whose line is short
 constexpr int A4_CTA_PLACES = 8;     // a CTA's stretch holds at least these
 constexpr float A4_LIFT = 8.f;           // probabilities are 2^8 times their share of the reference's
@@ -724,7 +724,7 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) att
 
 // Joins the parts of a problem (request, KV head, group) that stretches share, in their order; a CTA per problem and slice of its numbers.
 // With few problems of many parts a problem's numbers are cut into slices, so that more CTAs read (8 problems of 32768 rows, 74 parts each:
-// one CTA per problem took longer than the attention).  Each number's parts are dealt to SHARE threads.
+// one CTA per problem took longer than the attention itself).  Each number's parts are dealt to SHARE threads.
 constexpr int A4_MERGE_THREADS = 256;
 constexpr int A4_MERGE_PARTS = 64;       // parts whose shares are held at a time
 template <typename T, int D, int NT, int SLICES>
@@ -755,8 +755,16 @@ __global__ void __launch_bounds__(A4_MERGE_THREADS) attend4_merge_kernel(const _
     auto slot = [&](int i) { return i == 0 ? slot0 : 2 * (c0 + i); };
     const float2 *ml = reinterpret_cast<const float2 *>(a.part + (int64_t)2 * ctas_launched * N * D);
     const int v = threadIdx.x % N, r = threadIdx.x / N;
+    // (reads of many parts are asked for eight at a time: one after the other each would take the time of a trip to L2)
+    constexpr int AHEAD = SLICES > 1 ? 8 : 1;
     float m = -INFINITY;
-    for (int i = r; i < count; i += ROWS) m = fmaxf(m, ml[slot(i) * N + v].x);
+    for (int i = r; i < count; i += AHEAD * ROWS) {
+        float x[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) x[k] = i + k * ROWS < count ? ml[slot(i + k * ROWS) * N + v].x : -INFINITY;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) m = fmaxf(m, x[k]);
+    }
     top[r][v] = m;
     __syncthreads();
 #pragma unroll
@@ -767,20 +775,33 @@ __global__ void __launch_bounds__(A4_MERGE_THREADS) attend4_merge_kernel(const _
     for (int e = 0; e < EACH; ++e) den[e] = acc[e] = 0.f;
     for (int i0 = 0; i0 < count; i0 += A4_MERGE_PARTS) {
         const int here = min(A4_MERGE_PARTS, count - i0);
-        for (int i = r; i < here; i += ROWS) {
-            const float2 x = ml[slot(i0 + i) * N + v];
+#pragma unroll
+        for (int k = 0; k < (A4_MERGE_PARTS + ROWS - 1) / ROWS; ++k) {
+            const int i = r + k * ROWS;
+            if (i >= A4_MERGE_PARTS) continue;
+            const float2 x = i < here ? ml[slot(i0 + i) * N + v] : make_float2(-INFINITY, 0.f);
             share[i][v] = x.x == -INFINITY ? 0.f : exp2_fast(x.x - m);
             den_of[i][v] = x.y;
         }
         __syncthreads();
-#pragma unroll 8
-        for (int i = sub; i < here; i += SHARE) {
-            const float *from = a.part + slot(i0 + i) * N * D + x0;
+        constexpr int BATCH = SLICES > 1 ? 8 : EACH > 4 ? 2 : 4;
+        for (int i = sub; i < here; i += BATCH * SHARE) {
+            float x[BATCH][EACH];
 #pragma unroll
-            for (int e = 0; e < EACH; ++e) {
-                const int ve = (x0 + e * A4_MERGE_THREADS) / D;
-                acc[e] = fmaf(from[e * A4_MERGE_THREADS], share[i][ve], acc[e]);
-                den[e] = fmaf(den_of[i][ve], share[i][ve], den[e]);
+            for (int k = 0; k < BATCH; ++k)
+#pragma unroll
+                for (int e = 0; e < EACH; ++e)
+                    x[k][e] = i + k * SHARE < here ? a.part[slot(i0 + i + k * SHARE) * N * D + x0 + e * A4_MERGE_THREADS] : 0.f;
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const int at = min(i + k * SHARE, A4_MERGE_PARTS - 1);
+                if (i + k * SHARE >= here) continue;
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) {
+                    const int ve = (x0 + e * A4_MERGE_THREADS) / D;
+                    acc[e] = fmaf(x[k][e], share[at][ve], acc[e]);
+                    den[e] = fmaf(den_of[at][ve], share[at][ve], den[e]);
+                }
             }
         }
         __syncthreads();
@@ -868,9 +889,11 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
     const int64_t places = problems * (A4_START + (a.n_kv + A4_TILE - 1) / A4_TILE);
     const int grid = stretches(places, per_sm * device_sm_count());
     ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)grid), dim3(A4_THREADS), smem, st, a));
-    constexpr int MANY = C::N * D / 128;                         // slices of 128 numbers where the problems alone are few
-    auto join = problems * MANY <= 2 * device_sm_count() ? attend4_merge_kernel<T, D, NT, MANY> : attend4_merge_kernel<T, D, NT, 1>;
-    const dim3 join_grid((unsigned)problems, problems * MANY <= 2 * device_sm_count() ? MANY : 1);
+    // slices of 32 or 128 numbers where the problems alone are few
+    constexpr int FINE = C::N * D / 32, COARSE = C::N * D / 128;
+    const int slices = problems * FINE <= 2 * device_sm_count() ? FINE : problems * COARSE <= 2 * device_sm_count() ? COARSE : 1;
+    auto join = slices == FINE ? attend4_merge_kernel<T, D, NT, FINE> : slices == COARSE ? attend4_merge_kernel<T, D, NT, COARSE> : attend4_merge_kernel<T, D, NT, 1>;
+    const dim3 join_grid((unsigned)problems, (unsigned)slices);
     ELM_CUDA_TRY(launch_after(join, join_grid, dim3(A4_MERGE_THREADS), (a.batch + 1) * 8, st, a, grid, max_groups));
     count_launches(2);
     return cuda_status(cudaGetLastError());
