@@ -16,5 +16,6 @@ _BINDING_NAMES = {
 def __getattr__(name):
     if name in _BINDING_NAMES:
         from . import binding
-        return getattr(binding, name)
+        value = globals()[name] = getattr(binding, name)        # (found once: the next look-up does not come here)
+        return value
     raise AttributeError(name)

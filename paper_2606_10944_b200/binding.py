@@ -436,22 +436,13 @@ def attend_static_status(Q, K, n_core: int, precision="fp32") -> int:
 # ------------------------------------------------------------------------------------------------
 # rotary positions, pages, rows held in 4 bits
 # ------------------------------------------------------------------------------------------------
-class _On:
-    """The calls below run on their tensors' device, on its current stream, whatever the current device is: ``with _On(device)``."""
+# The calls below run on their tensors' device, on its current stream, whatever the current device is: one that finds another current
+# device calls itself again under that of its tensors.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
-    __slots__ = ("index", "other")
 
-    def __init__(self, index):
-        self.index, self.other = index, None
-
-    def __enter__(self):
-        if torch.cuda.current_device() != self.index:
-            self.other = torch.cuda.device(self.index)
-            self.other.__enter__()
-
-    def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
+def _stream_of(device: int) -> int:
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def _device(first, *tensors):
@@ -537,45 +528,48 @@ def rope(X, positions, rope: Rope, inverse=False, out=None):
     """elm_rope: X [B, H, n, d] (any strides, a head's numbers side by side) rotated by positions, an int32 tensor [B, n] or the first
     position of every sequence; ``inverse``: rotated back (the gradient).  ``out``: X itself, or another tensor of its shape."""
     tensor = isinstance(positions, torch.Tensor)
-    with _On(_device(X, out, positions if tensor else None)):
-        key = (X.shape, X.stride(), X.dtype, inverse, positions.shape if tensor else None)
+    device = _device(X, out, positions if tensor else None)
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _rope_again(X, positions, rope, inverse, out)
+    key = (X.shape, X.stride(), X.dtype, inverse, positions.shape if tensor else None)
+    if out is not None:
+        key += (out.shape, out.stride(), out.dtype)
+    p = rope._kept.get(key)
+    if p is None:
+        Y, xs = _rows(X, 4, "X")
+        if Y is not X:                                      # (a broadcast of one row)
+            if out is X:
+                raise ElmError("out: rows must lie apart")
+            return _rope_again(Y, positions, rope, inverse, out)
+        B, H, n, d = X.shape
         if out is not None:
-            key += (out.shape, out.stride(), out.dtype)
-        p = rope._kept.get(key)
-        if p is None:
-            Y, xs = _rows(X, 4, "X")
-            if Y is not X:                                      # (a broadcast of one row)
-                return _rope_of_copy(X, Y, positions, rope, inverse, out)
-            B, H, n, d = X.shape
-            if out is not None:
-                if out.shape != X.shape or out.dtype != X.dtype:
-                    raise ElmError("out must have X's shape and dtype")
-                os_ = out.stride()
-                if (os_[-1] != 1 and d > 1) or not any(os_[:-1]) and out.numel() > d:
-                    raise ElmError("out: the numbers of a head must lie side by side, rows apart")
-            if tensor:
-                _int32(positions, "positions", (B, n))
-            p = RopeParams(B, H, n, d, _storage_code(X), rope.rotary_dim, rope.layout, int(bool(inverse)), rope.scale, rope._freq_ptr)
-            p.x_stride[:] = xs[:3]
-            p.out_stride[:] = os_[:3] if out is not None else (0, 0, 0)
-            rope._kept.keep(key, p)
+            if out.shape != X.shape or out.dtype != X.dtype:
+                raise ElmError("out must have X's shape and dtype")
+            os_ = out.stride()
+            if (os_[-1] != 1 and d > 1) or not any(os_[:-1]) and out.numel() > d:
+                raise ElmError("out: the numbers of a head must lie side by side, rows apart")
         if tensor:
-            if positions.dtype is not torch.int32 or not positions.is_contiguous():
-                raise ElmError("positions must be a contiguous int32 tensor")
-            pos, first = positions.data_ptr(), 0
-        else:
-            pos, first = None, int(positions)
-        O = out if out is not None else torch.empty_like(X, memory_format=torch.contiguous_format)
-        rc = load_library().elm_rope(X.data_ptr(), pos, first, p, O.data_ptr(), _stream())
+            _int32(positions, "positions", (B, n))
+        p = RopeParams(B, H, n, d, _storage_code(X), rope.rotary_dim, rope.layout, int(bool(inverse)), rope.scale, rope._freq_ptr)
+        p.x_stride[:] = xs[:3]
+        p.out_stride[:] = os_[:3] if out is not None else (0, 0, 0)
+        rope._kept.keep(key, p)
+    if tensor:
+        if positions.dtype is not torch.int32 or not positions.is_contiguous():
+            raise ElmError("positions must be a contiguous int32 tensor")
+        pos, first = positions.data_ptr(), 0
+    else:
+        pos, first = None, int(positions)
+    O = out if out is not None else torch.empty_like(X, memory_format=torch.contiguous_format)
+    rc = load_library().elm_rope(X.data_ptr(), pos, first, p, O.data_ptr(), _stream_of(device))
     if rc:
         _check(rc, "elm_rope")
     return O
 
 
-def _rope_of_copy(X, Y, positions, rope_, inverse, out):
-    if out is X:
-        raise ElmError("out: rows must lie apart")
-    return rope(Y, positions, rope_, inverse, out)
+def _rope_again(X, positions, turn, inverse, out):              # (where ``rope`` is the name of an argument)
+    return rope(X, positions, turn, inverse, out)
 
 
 class PagePlan:
@@ -590,31 +584,34 @@ _plan_kept = _Kept()
 def page_plan(table, length, n_new, free, free_count, page_rows: int, max_tokens: int, length_out=None, free_count_out=None) -> PagePlan:
     """elm_page_plan: pages, positions and slots of the n_new [B] tokens that come to requests of length [B].  ``table`` [B, max_pages]
     gets the new pages' numbers; length_out and free_count_out may be length and free_count."""
-    with _On(_device(table, length, n_new, free, free_count, length_out, free_count_out)):
-        key = (table.shape, length.shape, n_new.shape, free.shape, free_count.shape, page_rows, max_tokens)
-        kept = _plan_kept.get(key)
-        if kept is None:
-            if table.dim() != 2:
-                raise ElmError("table must be [B, max_pages]")
-            B, max_pages = table.shape
-            _int32(length, "length", (B,)), _int32(n_new, "n_new", (B,)), _int32(free, "free"), _int32(free_count, "free_count", (1,))
-            # (one allocation for all that comes out)
-            sizes = [max(0, max_tokens), max(0, max_tokens), B, B, B + 1, 1]
-            kept = _plan_kept.keep(key, (PageParams(B, max_pages, page_rows, max_tokens, free.numel()), sum(sizes), sizes))
-        p, total, cuts = kept
-        for t in (table, length, n_new, free, free_count):
-            if t.dtype is not torch.int32 or not t.is_contiguous():
-                raise ElmError("table, length, n_new, free and free_count must be contiguous int32 tensors")
-        buf = torch.empty(total, dtype=torch.int32, device=table.device)
-        r = PagePlan()
-        r.positions, r.slots, r.start, r.length, r.cu, r.free_count = buf.split_with_sizes(cuts)
-        if length_out is not None:
-            r.length = _int32(length_out, "length_out", length.shape)
-        if free_count_out is not None:
-            r.free_count = _int32(free_count_out, "free_count_out", (1,))
-        rc = load_library().elm_page_plan(table.data_ptr(), length.data_ptr(), n_new.data_ptr(), free.data_ptr(), free_count.data_ptr(), p,
-                                          r.start.data_ptr(), r.length.data_ptr(), r.free_count.data_ptr(), r.cu.data_ptr(),
-                                          r.positions.data_ptr(), r.slots.data_ptr(), _stream())
+    device = _device(table, length, n_new, free, free_count, length_out, free_count_out)
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return page_plan(table, length, n_new, free, free_count, page_rows, max_tokens, length_out, free_count_out)
+    key = (table.shape, length.shape, n_new.shape, free.shape, free_count.shape, page_rows, max_tokens)
+    kept = _plan_kept.get(key)
+    if kept is None:
+        if table.dim() != 2:
+            raise ElmError("table must be [B, max_pages]")
+        B, max_pages = table.shape
+        _int32(length, "length", (B,)), _int32(n_new, "n_new", (B,)), _int32(free, "free"), _int32(free_count, "free_count", (1,))
+        # (one allocation for all that comes out)
+        sizes = [max(0, max_tokens), max(0, max_tokens), B, B, B + 1, 1]
+        kept = _plan_kept.keep(key, (PageParams(B, max_pages, page_rows, max_tokens, free.numel()), sum(sizes), sizes))
+    p, total, cuts = kept
+    for t in (table, length, n_new, free, free_count):
+        if t.dtype is not torch.int32 or not t.is_contiguous():
+            raise ElmError("table, length, n_new, free and free_count must be contiguous int32 tensors")
+    buf = torch.empty(total, dtype=torch.int32, device=table.device)
+    r = PagePlan()
+    r.positions, r.slots, r.start, r.length, r.cu, r.free_count = buf.split_with_sizes(cuts)
+    if length_out is not None:
+        r.length = _int32(length_out, "length_out", length.shape)
+    if free_count_out is not None:
+        r.free_count = _int32(free_count_out, "free_count_out", (1,))
+    rc = load_library().elm_page_plan(table.data_ptr(), length.data_ptr(), n_new.data_ptr(), free.data_ptr(), free_count.data_ptr(), p,
+                                      r.start.data_ptr(), r.length.data_ptr(), r.free_count.data_ptr(), r.cu.data_ptr(),
+                                      r.positions.data_ptr(), r.slots.data_ptr(), _stream_of(device))
     if rc:
         _check(rc, "elm_page_plan")
     return r
@@ -623,12 +620,13 @@ def page_plan(table, length, n_new, free, free_count, page_rows: int, max_tokens
 def page_release(table, length, done, free, free_count, page_rows: int):
     """elm_page_release: the pages of the requests with done [B] != 0 go back to the end of free; everything in place."""
     lib = load_library()
-    with _On(_device(table, length, done, free, free_count)):
+    device = _device(table, length, done, free, free_count)
+    with torch.cuda.device(device):
         B, max_pages = _int32(table, "table").shape
         _int32(length, "length", (B,)), _int32(done, "done", (B,)), _int32(free, "free"), _int32(free_count, "free_count", (1,))
         p = PageParams(B, max_pages, page_rows, 0, free.numel())
         _check(lib.elm_page_release(table.data_ptr(), length.data_ptr(), done.data_ptr(), free.data_ptr(), free_count.data_ptr(),
-                                    ctypes.byref(p), _stream()), "elm_page_release")
+                                    ctypes.byref(p), _stream_of(device)), "elm_page_release")
 
 
 def cache4_row_bytes(d: int) -> int:
@@ -657,59 +655,62 @@ _append_kept = _Kept()
 def cache4_append(rows, K, V, slots, rope: Rope = None, positions=None, Q=None, q_out=None):
     """elm_cache4_append: K, V [T, Hkv, d] into the pool's rows slots [T] (a slot outside the pool: passed over), keys rotated by
     ``rope`` at positions [T].  Q [T, Hq, d] comes back rotated (in q_out, which may be Q; of tokens passed over, as q_out was)."""
-    with _On(_device(rows, K, V, slots, positions, Q, q_out)):
-        kept = _append_kept if rope is None else rope._kept
-        key = (rows.shape, K.shape, K.stride(), K.dtype, V.shape, V.stride(), V.dtype, slots.shape)
-        if positions is not None:
-            key += (positions.shape,)
-        if Q is not None:
-            key += (Q.shape, Q.stride(), Q.dtype)
-            if q_out is not None:
-                key += (q_out.shape, q_out.stride(), q_out.dtype)
-        p = kept.get(key)
-        if p is None:
-            d = _pool_d(rows)
-            K2, ks = _rows(K, 3, "K")
-            V2, vs = _rows(V, 3, "V")
-            Q2, qs = (None, None) if Q is None else _rows(Q, 3, "Q")
-            if K2 is not K or V2 is not V or Q2 is not Q:       # (a broadcast of one row)
-                if Q2 is not Q and q_out is Q:
-                    raise ElmError("q_out: rows must lie apart")
-                return cache4_append(rows, K2, V2, slots, rope, positions, Q2, q_out)
-            T, H = K.shape[:2]
-            if K.shape != V.shape or K.dtype != V.dtype or K.shape[2] != d or H != rows.shape[1]:
-                raise ElmError("K and V must be [tokens, kv_heads, d] of the pool's heads, of one dtype")
-            _int32(slots, "slots", (T,))
-            if rope is not None:
-                if positions is None:
-                    raise ElmError("a rotation needs positions")
-                _int32(positions, "positions", (T,))
-            p = AppendParams(T, 0, H, d, _storage_code(K), rows.shape[2], rows.shape[0])
-            if rope is not None:
-                p.rotary_dim, p.layout, p.scale, p.inv_freq = rope.rotary_dim, rope.layout, rope.scale, rope._freq_ptr
-            p.k_stride[:] = ks[:2]
-            p.v_stride[:] = vs[:2]
-            if Q is not None:
-                if Q.shape[0] != T or Q.shape[2] != d or Q.dtype != K.dtype:
-                    raise ElmError("Q must be [tokens, q_heads, d] of K's dtype")
-                p.q_heads = Q.shape[1]
-                p.q_stride[:] = qs[:2]
-                if q_out is not None:
-                    if q_out.shape != Q.shape or q_out.dtype != Q.dtype or q_out.stride(2) != 1:
-                        raise ElmError("q_out must have Q's shape and dtype, the numbers of a head side by side")
-                    if not any(q_out.stride()[:2]) and q_out.numel() > d:
-                        raise ElmError("q_out: rows must lie apart")
-                    p.q_out_stride[:] = q_out.stride()[:2]
-            kept.keep(key, p)
-        if rows.dtype is not torch.uint8 or not rows.is_contiguous() or slots.dtype is not torch.int32 or not slots.is_contiguous():
-            raise ElmError("rows must be contiguous uint8 and slots contiguous int32")
-        pos = None
+    device = _device(rows, K, V, slots, positions, Q, q_out)
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return cache4_append(rows, K, V, slots, rope, positions, Q, q_out)
+    kept = _append_kept if rope is None else rope._kept
+    key = (rows.shape, K.shape, K.stride(), K.dtype, V.shape, V.stride(), V.dtype, slots.shape)
+    if positions is not None:
+        key += (positions.shape,)
+    if Q is not None:
+        key += (Q.shape, Q.stride(), Q.dtype)
+        if q_out is not None:
+            key += (q_out.shape, q_out.stride(), q_out.dtype)
+    p = kept.get(key)
+    if p is None:
+        d = _pool_d(rows)
+        K2, ks = _rows(K, 3, "K")
+        V2, vs = _rows(V, 3, "V")
+        Q2, qs = (None, None) if Q is None else _rows(Q, 3, "Q")
+        if K2 is not K or V2 is not V or Q2 is not Q:       # (a broadcast of one row)
+            if Q2 is not Q and q_out is Q:
+                raise ElmError("q_out: rows must lie apart")
+            return cache4_append(rows, K2, V2, slots, rope, positions, Q2, q_out)
+        T, H = K.shape[:2]
+        if K.shape != V.shape or K.dtype != V.dtype or K.shape[2] != d or H != rows.shape[1]:
+            raise ElmError("K and V must be [tokens, kv_heads, d] of the pool's heads, of one dtype")
+        _int32(slots, "slots", (T,))
         if rope is not None:
-            if positions.dtype is not torch.int32 or not positions.is_contiguous():
-                raise ElmError("positions must be contiguous int32")
-            pos = positions.data_ptr()
-        O = None if Q is None else q_out if q_out is not None else torch.empty_like(Q, memory_format=torch.contiguous_format)
-        rc = load_library().elm_cache4_append(_ptr(Q), K.data_ptr(), V.data_ptr(), pos, slots.data_ptr(), p, _ptr(O), rows.data_ptr(), _stream())
+            if positions is None:
+                raise ElmError("a rotation needs positions")
+            _int32(positions, "positions", (T,))
+        p = AppendParams(T, 0, H, d, _storage_code(K), rows.shape[2], rows.shape[0])
+        if rope is not None:
+            p.rotary_dim, p.layout, p.scale, p.inv_freq = rope.rotary_dim, rope.layout, rope.scale, rope._freq_ptr
+        p.k_stride[:] = ks[:2]
+        p.v_stride[:] = vs[:2]
+        if Q is not None:
+            if Q.shape[0] != T or Q.shape[2] != d or Q.dtype != K.dtype:
+                raise ElmError("Q must be [tokens, q_heads, d] of K's dtype")
+            p.q_heads = Q.shape[1]
+            p.q_stride[:] = qs[:2]
+            if q_out is not None:
+                if q_out.shape != Q.shape or q_out.dtype != Q.dtype or q_out.stride(2) != 1:
+                    raise ElmError("q_out must have Q's shape and dtype, the numbers of a head side by side")
+                if not any(q_out.stride()[:2]) and q_out.numel() > d:
+                    raise ElmError("q_out: rows must lie apart")
+                p.q_out_stride[:] = q_out.stride()[:2]
+        kept.keep(key, p)
+    if rows.dtype is not torch.uint8 or not rows.is_contiguous() or slots.dtype is not torch.int32 or not slots.is_contiguous():
+        raise ElmError("rows must be contiguous uint8 and slots contiguous int32")
+    pos = None
+    if rope is not None:
+        if positions.dtype is not torch.int32 or not positions.is_contiguous():
+            raise ElmError("positions must be contiguous int32")
+        pos = positions.data_ptr()
+    O = None if Q is None else q_out if q_out is not None else torch.empty_like(Q, memory_format=torch.contiguous_format)
+    rc = load_library().elm_cache4_append(_ptr(Q), K.data_ptr(), V.data_ptr(), pos, slots.data_ptr(), p, _ptr(O), rows.data_ptr(), _stream_of(device))
     if rc:
         _check(rc, "elm_cache4_append")
     return O
@@ -727,29 +728,32 @@ _cache4_kept = _Kept()
 def cache4_read(rows, table, n: int, idx=None, length=None, dtype=torch.bfloat16, out=None):
     """elm_cache4_read -> K, V [B, Hkv, n, d]: rows 0 .. n - 1 of every request, or rows idx [B, Hkv, n]; a row that is not there (past
     length [B], on no page) is zeros.  ``out``: a pair of tensors for them."""
-    with _On(_device(rows, table, idx, length, *(out or ()))):
-        key = (rows.shape, table.shape, n, idx if idx is None else idx.shape, length if length is None else length.shape, dtype)
-        kept = _cache4_kept.get(key)
-        if kept is None:
-            code = {torch.float32: ELM_F32, torch.bfloat16: ELM_BF16}.get(dtype)
-            if code is None:
-                raise ElmError(f"unsupported dtype {dtype}")
-            p = _cache4_params(rows, table, rows.shape[1], code, n)
-            shape = (p.batch, p.kv_heads, n, p.d)
-            if idx is not None:
-                _int32(idx, "idx", shape[:3])
-            if length is not None:
-                _int32(length, "length", shape[:1])
-            kept = _cache4_kept.keep(key, (p, shape))
-        p, shape = kept
-        _int32_all(rows, table, idx, length)
-        if out is not None:
-            K, V = out
-            if any(tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() for t in out):
-                raise ElmError(f"out must be two contiguous tensors of shape {shape} and dtype {dtype}")
-        else:
-            K, V = torch.empty(shape, dtype=dtype, device=rows.device), torch.empty(shape, dtype=dtype, device=rows.device)
-        rc = load_library().elm_cache4_read(rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(idx), p, K.data_ptr(), V.data_ptr(), _stream())
+    device = _device(rows, table, idx, length, *(out or ()))
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return cache4_read(rows, table, n, idx, length, dtype, out)
+    key = (rows.shape, table.shape, n, idx if idx is None else idx.shape, length if length is None else length.shape, dtype)
+    kept = _cache4_kept.get(key)
+    if kept is None:
+        code = {torch.float32: ELM_F32, torch.bfloat16: ELM_BF16}.get(dtype)
+        if code is None:
+            raise ElmError(f"unsupported dtype {dtype}")
+        p = _cache4_params(rows, table, rows.shape[1], code, n)
+        shape = (p.batch, p.kv_heads, n, p.d)
+        if idx is not None:
+            _int32(idx, "idx", shape[:3])
+        if length is not None:
+            _int32(length, "length", shape[:1])
+        kept = _cache4_kept.keep(key, (p, shape))
+    p, shape = kept
+    _int32_all(rows, table, idx, length)
+    if out is not None:
+        K, V = out
+        if any(tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() for t in out):
+            raise ElmError(f"out must be two contiguous tensors of shape {shape} and dtype {dtype}")
+    else:
+        K, V = torch.empty(shape, dtype=dtype, device=rows.device), torch.empty(shape, dtype=dtype, device=rows.device)
+    rc = load_library().elm_cache4_read(rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(idx), p, K.data_ptr(), V.data_ptr(), _stream_of(device))
     if rc:
         _check(rc, "elm_cache4_read")
     return K, V
@@ -819,25 +823,27 @@ def cache4_attend(Q, rows, table, length=None, idx=None, w=None, cu=None, max_q=
     of the lengths that the host knows; causal: a request's queries are its last tokens), or the list idx with weights w
     [B, Hkv, n_core].  With cu [B + 1]: Q [T, Hq, d], request b has the tokens cu[b] .. cu[b + 1] - 1, max_q at most.  O like Q."""
     device = _device(rows, Q, table, length, idx, w, cu, workspace, out)
-    with _On(device):
-        key = (device, Q.shape, Q.stride(), Q.dtype, rows.shape, table.shape, max_q, n_kv, causal,
-               length if length is None else length.shape, cu if cu is None else cu.shape,
-               idx if idx is None else (idx.shape, w if w is None else (w.shape, w.dtype, w.is_contiguous())),
-               out if out is None else (out.shape, out.stride(), out.dtype))
-        kept = _cache4_kept.get(key)
-        if kept is None:
-            p = _attend4_params(Q, rows, table, cu, idx, w, length, n_kv, max_q, causal, out)
-            if p is None:
-                if out is Q:
-                    raise ElmError("out: rows must lie apart")
-                return cache4_attend(Q.contiguous(), rows, table, length, idx, w, cu, max_q, n_kv, causal, workspace, out)
-            kept = _cache4_kept.keep(key, (p, cache4_attend_workspace_bytes(p, idx is not None)))
-        p, need = kept
-        _int32_all(rows, table, length, idx, cu)
-        ws = workspace if workspace is not None else torch.empty(need, dtype=torch.uint8, device=Q.device)
-        O = out if out is not None else torch.empty_like(Q, memory_format=torch.contiguous_format)
-        rc = load_library().elm_cache4_attend(Q.data_ptr(), rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(cu), _ptr(idx), _ptr(w), p,
-                                              O.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return cache4_attend(Q, rows, table, length, idx, w, cu, max_q, n_kv, causal, workspace, out)
+    key = (device, Q.shape, Q.stride(), Q.dtype, rows.shape, table.shape, max_q, n_kv, causal,
+           length if length is None else length.shape, cu if cu is None else cu.shape,
+           idx if idx is None else (idx.shape, w if w is None else (w.shape, w.dtype, w.is_contiguous())),
+           out if out is None else (out.shape, out.stride(), out.dtype))
+    kept = _cache4_kept.get(key)
+    if kept is None:
+        p = _attend4_params(Q, rows, table, cu, idx, w, length, n_kv, max_q, causal, out)
+        if p is None:
+            if out is Q:
+                raise ElmError("out: rows must lie apart")
+            return cache4_attend(Q.contiguous(), rows, table, length, idx, w, cu, max_q, n_kv, causal, workspace, out)
+        kept = _cache4_kept.keep(key, (p, cache4_attend_workspace_bytes(p, idx is not None)))
+    p, need = kept
+    _int32_all(rows, table, length, idx, cu)
+    ws = workspace if workspace is not None else torch.empty(need, dtype=torch.uint8, device=Q.device)
+    O = out if out is not None else torch.empty_like(Q, memory_format=torch.contiguous_format)
+    rc = load_library().elm_cache4_attend(Q.data_ptr(), rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(cu), _ptr(idx), _ptr(w), p,
+                                          O.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(device))
     if rc:
         _check(rc, "elm_cache4_attend")
     return O

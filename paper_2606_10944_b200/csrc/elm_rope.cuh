@@ -22,8 +22,8 @@ inline bool rope_turns(const double *inv_freq, int pairs, RopeTurns &out)
     for (int i = 0; i < pairs; ++i) {
         if (!isfinite(inv_freq[i])) return false;
         // (long double carries 64 bits here: the fraction is as good as its 64 bits hold)
-        long double f = (long double)inv_freq[i] / 6.283185307179586476925286766559005768L;
-        f -= floorl(f);
+        long double f = (long double)inv_freq[i] * 0.159154943091895335768883763372514362L;      // 1 / (2 pi)
+        if (!(f >= 0.0L && f < 1.0L)) f -= floorl(f);
         const long double scaled = f * 18446744073709551616.0L;
         out.turn[i] = scaled >= 18446744073709551615.0L ? ~0ull : (uint64_t)(scaled + 0.5L);
     }
