@@ -752,7 +752,8 @@ def cache4_read(rows, table, n: int, idx=None, length=None, dtype=torch.bfloat16
         if any(tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() for t in out):
             raise ElmError(f"out must be two contiguous tensors of shape {shape} and dtype {dtype}")
     else:
-        K, V = torch.empty(shape, dtype=dtype, device=rows.device), torch.empty(shape, dtype=dtype, device=rows.device)
+        K = torch.empty_strided(shape, (shape[1] * n * shape[3], n * shape[3], shape[3], 1), dtype=dtype, device=rows.device)
+        V = torch.empty_like(K)
     rc = load_library().elm_cache4_read(rows.data_ptr(), table.data_ptr(), _ptr(length), _ptr(idx), p, K.data_ptr(), V.data_ptr(), _stream_of(device))
     if rc:
         _check(rc, "elm_cache4_read")

@@ -338,18 +338,27 @@ def test_attend_list(dtype, d, n_core, n_q, rep):
     _check_list(pool, table, idx, w, Q, got, page, d)
 
 
+def _by_tensor_cores(Q, pool, table, n_core):
+    """Whether a call takes the tensor-core form, by the workspace it asks for."""
+    p = elm.Cache4Params(Q.shape[0], Q.shape[1], pool.shape[1], Q.shape[3], 1, pool.shape[2], pool.shape[0], table.shape[1], n_core, Q.shape[2])
+    need = elm.cache4_attend_workspace_bytes(p, True)
+    p.dtype = 0                                               # (fp32 queries do not)
+    return need != elm.cache4_attend_workspace_bytes(p, True)
+
+
 @pytest.mark.parametrize("d", [128, 64])
 @pytest.mark.parametrize("n_core", [1, 100, 128, 500])
 def test_attend_list_of_many_queries(d, n_core):
     """The tensor-core form of bf16 lists: probabilities are bf16 there (half a step 2^-8 of each)."""
     r = np.random.default_rng(n_core)
-    B, H, rep, page, n, n_q = 2, 2, 2, 64, 900, 300
+    B, H, rep, page, n, n_q = 2, 2, 2, 64, 900, 3001
     table, n_pages = _tables(r, [n] * B, page, 16)
     pool = _pool(r, n_pages, H, page, d)
     idx, w = _list(r, B, H, n, n_core)
     if n_core > 30:
         idx[0, 0, 3], w[1, 1, 9], idx[0, 0, 60] = -1, 0.0, 10 ** 9
     Q = torch.randn(B, H * rep, n_q, d, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    assert _by_tensor_cores(Q, pool, table, n_core)
     tw = torch.as_tensor(w, dtype=torch.float32).cuda()
     got = elm.cache4_attend(Q, pool, _ints(table), idx=_ints(idx), w=tw)
     for b in range(B):
@@ -363,6 +372,7 @@ def test_attend_list_of_many_queries(d, n_core):
             tol = plain.attend_bound(o, size, reach, most, torch.bfloat16, n_core) + (2.0 ** -8 + 2e-4) * size
             assert (err <= tol).all()
     # the same with few queries: the other form
+    assert not _by_tensor_cores(Q[:, :, :3], pool, table, n_core)
     few = elm.cache4_attend(Q[:, :, :3].contiguous(), pool, _ints(table), idx=_ints(idx), w=tw)
     assert (few.float() - got[:, :, :3].float()).abs().max() <= 0.05 * got.float().abs().max()
 
@@ -371,8 +381,9 @@ def test_attend_list_nothing_seen():
     r = np.random.default_rng(0)
     pool = _pool(r, 4, 1, 16, 128)
     idx, w = np.full((1, 1, 40), -1), np.ones((1, 1, 40))
-    for n_q in (1, 200):
+    for n_q in (1, 200, 20000):
         Q = torch.randn(1, 2, n_q, 128).bfloat16().cuda()
+        assert _by_tensor_cores(Q, pool, np.zeros((1, 2)), 40) == (n_q == 20000)
         got = elm.cache4_attend(Q, pool, _ints([[0, 1]]), idx=_ints(idx), w=torch.as_tensor(w, dtype=torch.float32).cuda())
         assert (got == 0).all()
 
@@ -500,11 +511,12 @@ def test_coreset_of_a_stored_prompt():
     table = _ints(order[None])
     k, v = elm.cache4_read(pool, table, n)
     idx, w = elm.compress(k, v, 8, 4, seed=5)
-    for n_q in (1, 5, 400):
+    for n_q in (1, 5, 400, 8000):
         Q = torch.randn(B, H * rep, n_q, d, generator=g).bfloat16().cuda()
         got, ref = elm.cache4_attend(Q, pool, table, idx=idx, w=w), elm.attend(Q, k, v, idx, w)
         # two bf16 outputs, and probabilities of 2^-8 in either, of values whose mean size is the bound's
         size = float(v.float().abs().mean()) * 4
         assert (got.float() - ref.float()).abs().max().item() <= 2 * 2.0 ** -8 * size * 2
+    assert _by_tensor_cores(Q, pool, table, 256)
     many = elm.cache4_attend(Q, pool, table, idx=idx, w=w)
     assert torch.equal(many, elm.attend(Q, k, v, idx, w))     # the same kernel over the same bf16 rows
