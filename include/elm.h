@@ -412,7 +412,9 @@ int elm_cache4_read(const void *rows, const int32_t *table, const int32_t *lengt
  *                        elm_page_plan), request b has the tokens cu[b] .. cu[b + 1] - 1 of Q and O; batch strides are not used.
  *   idx, w [batch][kv_heads][n_kv]  a weighted list of the request's rows, as elm_attend takes it; every query sees all of it.
  * Rows that are not there, and list entries whose weight is not above 0, are not seen, whatever they hold; a query that sees
- * nothing gets zeros.  Tokens of O outside cu, and those of requests without queries, are left as they were.
+ * nothing gets zeros.  Tokens of O outside cu, and those of requests without queries, are left as they were.  O may be Q with the
+ * same strides, else the two must not overlap.  (A request that elm_page_plan did not serve has queries in cu and its old
+ * length: what its tokens of O hold afterwards means nothing.)
  * dtype is that of Q and O: ELM_BF16 (probabilities rounded to fp16 for P V) or ELM_F32 (queries and probabilities as two fp16
  * parts); logits, maxima, denominators and accumulators are fp32 either way.  batch <= 1024.
  * bf16 lists met by many queries take the tensor-core kernel of elm_attend over a gathered bf16 copy (dense Q and O only).

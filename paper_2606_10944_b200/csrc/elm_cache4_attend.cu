@@ -35,8 +35,8 @@ constexpr int A4_WARPS = 4;
 constexpr int A4_THREADS = 32 * A4_WARPS;
 constexpr int A4_TILE = 32;              // rows of a warp's tile
 constexpr int A4_STAGES = 2;
-constexpr int A4_START = 16;              // what a problem's beginning and end cost, in tiles
-constexpr int A4_MAX_BATCH = 1024, A4_FEW = 127;                // requests of a call; of one whose line is short
+constexpr int A4_START = 12;              // what a problem's beginning and end cost, in tiles
+constexpr int A4_MAX_BATCH = 1024, A4_SOME = 511, A4_FEW = 127;                // requests of a call; of calls whose line is short
 constexpr int A4_CTA_PLACES = 8;     // a CTA's stretch holds at least these
 constexpr float A4_LIFT = 8.f;           // probabilities are 2^8 times their share of the reference's
 constexpr float A4_SLACK = 6.f;          // how far the maximum may pass the reference: fp16 ends at 2^16
@@ -52,29 +52,41 @@ struct Attend4Args {
     int32_t batch, q_heads, rep, n_kv, n_q, n_tokens, causal;
     int32_t cluster;                     // CTAs of the cluster that does a problem; 0: the line of tiles is cut into stretches
     int32_t max_groups;                  // groups of query vectors of a request at most
+    int32_t q_wide;                      // every row of Q starts on an 8-byte boundary
 };
 
 // Where the problems of every request begin in the line of tiles.  A request of n query vectors (rep * its tokens) over t tiles has
 // kv_heads * ceil(n / N) problems of A4_START + t places each, one after the other, KV head slowest.  The first A4_START places of a problem hold no
 // tile: they stand for what it costs whatever its length (48 requests of 1 .. 32768 rows, lengths spread over the logarithm: the CTAs that
 // met many short ones took 2.5 times as long as the others).
+// what is known of a request, and what follows from it
 struct Request {
-    int32_t tokens, first_token, rows, groups, tiles, places;
+    int32_t rows, tokens, first_token, groups, tiles, places;
 };
-__device__ __forceinline__ Request request_at(const Attend4Args &a, int b, int n_vec)
+__device__ __forceinline__ Request request_from(const Attend4Args &a, int4 known, int n_vec)
 {
     Request r;
-    r.first_token = a.cu ? a.cu[b] : 0;
-    r.tokens = a.cu ? a.cu[b + 1] - r.first_token : a.n_q;
-    if (a.cu) {                          // only tokens that Q has
-        if (r.first_token < 0 || r.tokens < 0) r.tokens = 0;
-        else if ((int64_t)r.first_token + r.tokens > a.n_tokens) r.tokens = max(0, a.n_tokens - r.first_token);
-        r.tokens = min(r.tokens, a.n_q);
-    }
-    r.rows = a.idx ? a.n_kv : min(max(a.length[b], 0), a.n_kv);
+    r.rows = known.x;
+    r.tokens = known.y;
+    r.first_token = known.z;
     r.groups = (r.tokens * a.rep + n_vec - 1) / n_vec;
     r.tiles = max(1, (r.rows + A4_TILE - 1) / A4_TILE);
     r.places = A4_START + r.tiles;
+    return r;
+}
+__device__ __forceinline__ int4 look_at_request(const Attend4Args &a, int b)
+{
+    int4 r = make_int4(a.n_kv, a.n_q, 0, 0);
+    if (!a.idx) r.x = a.length[b];
+    if (a.cu) {
+        r.z = a.cu[b];
+        r.y = a.cu[b + 1] - r.z;
+        // only tokens that Q has
+        if (r.z < 0 || r.y < 0) r.y = 0;
+        else if ((int64_t)r.z + r.y > a.n_tokens) r.y = max(0, a.n_tokens - r.z);
+        r.y = min(r.y, a.n_q);
+    }
+    r.x = min(max(r.x, 0), a.n_kv);
     return r;
 }
 
@@ -119,6 +131,9 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
+// shared memory of the line of tiles: a prefix and four words for each request
+constexpr int line_bytes(int batch) { return (batch + 2) * 8 + batch * 16; }
+
 template <int D, int NT, int PARTS> struct A4 {
     using R = Row4<D>;
     static constexpr int N = 8 * NT;
@@ -131,41 +146,51 @@ template <int D, int NT, int PARTS> struct A4 {
     static constexpr int OFF_ML = OFF_BIAS + A4_WARPS * A4_STAGES * A4_TILE * 4;
     static constexpr int OFF_QS = OFF_ML + A4_WARPS * N * 2 * 4;  // [N] scale of the logits of a vector
     static constexpr int OFF_Q = (OFF_QS + N * 4 + 15) / 16 * 16; // [PARTS][NT][KS / 2][32 lanes] 16 bytes
-    static constexpr int OFF_LINE = OFF_Q + PARTS * NT * (KS / 2) * 512;
-    static int total(int batch) { return OFF_LINE + (batch + 1) * 8; }
+    static constexpr int OFF_LINE = OFF_Q + PARTS * NT * (KS / 2) * 512;                   // (a multiple of 16)
+    static int total(int batch) { return OFF_LINE + line_bytes(batch); }
 };
 
-// prefix[b] = places before request b; every thread returns the total
+// prefix[b] = places before request b, known[b] = what is known of it; every thread returns the total.  The requests are looked at side by side,
+// then every thread adds up a run of them and the runs are summed in one scan.
+__device__ __forceinline__ int4 *line_known(int64_t *prefix, int batch) { return reinterpret_cast<int4 *>(prefix + ((batch + 2) & ~1)); }
 __device__ __forceinline__ int64_t lay_line(const Attend4Args &a, int n_vec, int64_t *prefix, int64_t *part)
 {
-    int64_t before = 0;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int b0 = 0; b0 < a.batch; b0 += blockDim.x) {
-        const int b = b0 + threadIdx.x;
-        int64_t mine = 0;
-        if (b < a.batch) {
-            const Request r = request_at(a, b, n_vec);
-            mine = (int64_t)a.pool.kv_heads * r.groups * r.places;
-        }
-        int64_t x = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
-        }
-        if (lane == 31) part[warp] = x;
-        __syncthreads();
-        int64_t add = before;
-        for (int i = 0; i < (int)(blockDim.x >> 5); ++i) {
-            if (i < warp) add += part[i];
-            before += part[i];
-        }
-        if (b < a.batch) prefix[b] = add + x - mine;
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) prefix[a.batch] = before;
+    int4 *known = line_known(prefix, a.batch);
+    for (int b = threadIdx.x; b < a.batch; b += blockDim.x) known[b] = look_at_request(a, b);
     __syncthreads();
-    return before;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, run = (a.batch + blockDim.x - 1) / blockDim.x;
+    const int b0 = min(a.batch, (int)threadIdx.x * run), b1 = min(a.batch, b0 + run);
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) {
+        const Request r = request_from(a, known[b], n_vec);
+        mine += (int64_t)(a.pool.kv_heads * r.groups) * r.places;
+    }
+    int64_t x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 31) part[warp] = x;
+    __syncthreads();
+    int64_t total = 0, at = x - mine;
+    for (int i = 0; i < (int)(blockDim.x >> 5); ++i) {
+        if (i < warp) at += part[i];
+        total += part[i];
+    }
+    for (int b = b0; b < b1; ++b) {
+        const Request r = request_from(a, known[b], n_vec);
+        prefix[b] = at;
+        at += (int64_t)(a.pool.kv_heads * r.groups) * r.places;
+    }
+    if (threadIdx.x == 0) prefix[a.batch] = total;
+    __syncthreads();
+    return total;
+}
+// a / b and a * b / c of numbers that are mostly small: a division of 64 bits takes several times as long
+__device__ __forceinline__ int64_t div_small(int64_t x, int64_t y)
+{
+    return ((uint64_t)x | (uint64_t)y) >> 32 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
 }
 __host__ __device__ __forceinline__ int stretches(int64_t total, int ctas)
 {
@@ -212,14 +237,14 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) att
         const int64_t total = lay_line(a, N, prefix, reinterpret_cast<int64_t *>(smem));
         const int ctas = stretches(total, gridDim.x);
         if ((int)blockIdx.x >= ctas) return;
-        begin = total * blockIdx.x / ctas;
-        end = total * (blockIdx.x + 1) / ctas;
+        begin = div_small(total * blockIdx.x, ctas);
+        end = div_small(total * (blockIdx.x + 1), ctas);
         b = request_of(prefix, a.batch, begin);
     }
     for (int64_t f = begin; f < end;) {
         if (!a.cluster)
             while (prefix[b + 1] <= f) ++b;
-        const Request rq = request_at(a, b, N);
+        const Request rq = request_from(a, a.cluster ? look_at_request(a, b) : line_known(prefix, a.batch)[b], N);
         int h, group, tile0, tile1;
         const bool first_segment = f == begin;
         if (a.cluster) {
@@ -233,7 +258,7 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) att
             tile1 = (int)((int64_t)rq.tiles * (rank + 1) / a.cluster);
         } else {
             const int64_t in_request = f - prefix[b];
-            const int problem = (int)(in_request / rq.places), place0 = (int)(in_request - (int64_t)problem * rq.places);
+            const int problem = (int)div_small(in_request, rq.places), place0 = (int)(in_request - (int64_t)problem * rq.places);
             const int place1 = (int)min((int64_t)rq.places, place0 + (end - f));
             f += place1 - place0;
             tile0 = max(0, place0 - A4_START);
@@ -250,6 +275,31 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) att
         const int last_seen = tail ? rq.rows - rq.tokens + 1 + (vec0 + vectors - 1) / a.rep : rq.rows;
         const int first_seen = tail ? rq.rows - rq.tokens + 1 + vec0 / a.rep : rq.rows;
         const int tile_end = min(tile1, (last_seen + A4_TILE - 1) / A4_TILE);
+
+        // ---- the queries are asked for first: vector q_vec by PER threads ----
+        constexpr int PER = A4_THREADS / N, EACH = D / PER;      // threads to a vector, numbers to a thread
+        const int q_vec = threadIdx.x / PER, q_sub = threadIdx.x % PER;
+        uint32_t q_raw[EACH * sizeof(T) / 4];
+#pragma unroll
+        for (int i = 0; i < (int)(EACH * sizeof(T) / 4); ++i) q_raw[i] = 0u;
+        if (q_vec < vectors) {
+            const int vv = vec0 + q_vec, tok = vv / a.rep, head = h * a.rep + vv % a.rep;
+            const T *src = (const T *)a.q + (a.cu ? (int64_t)(rq.first_token + tok) * a.qs[2] : b * a.qs[0] + tok * a.qs[2]) + head * a.qs[1] + q_sub * EACH;
+            if (a.q_wide) {
+#pragma unroll
+                for (int i = 0; i < (int)(EACH * sizeof(T) / 8); ++i) {
+                    const uint2 w = reinterpret_cast<const uint2 *>(src)[i];
+                    q_raw[2 * i] = w.x;
+                    q_raw[2 * i + 1] = w.y;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) {
+                    if constexpr (sizeof(T) == 2) q_raw[i / 2] |= (uint32_t)__bfloat16_as_ushort(src[i]) << (16 * (i & 1));
+                    else q_raw[i] = __float_as_uint(src[i]);
+                }
+            }
+        }
 
         // ---- the rows of this warp's tiles, looked up a tile before they are fetched ----
         uint32_t next_row[2] = {NO_ROW, NO_ROW};                 // LIST: [0] is lane's row of the tile; else the first rows of its halves
@@ -325,35 +375,27 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) att
             look_up(++ahead);
         }
 
-        // ---- queries: vector v by the threads of a 16th of the CTA; scaled by a power of two, laid out as the lanes want them ----
+        // ---- queries: scaled by a power of two, laid out as the lanes want them ----
         {
-            constexpr int PER = A4_THREADS / N, EACH = D / PER;  // threads to a vector, numbers to a thread
-            const int v = threadIdx.x / PER, sub = threadIdx.x % PER;
-            const int vv = vec0 + v, tok = vv / a.rep, head = h * a.rep + vv % a.rep;
             float x[EACH];
             float top = 0.f;
-            if (v < vectors) {
-                const T *src = (const T *)a.q + (a.cu ? (int64_t)(rq.first_token + tok) * a.qs[2] : b * a.qs[0] + tok * a.qs[2]) + head * a.qs[1];
 #pragma unroll
-                for (int i = 0; i < EACH; ++i) {
-                    x[i] = load_as<float>(src, sub * EACH + i);
-                    top = fmaxf(top, fabsf(x[i]));
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < EACH; ++i) x[i] = 0.f;
+            for (int i = 0; i < EACH; ++i) {
+                if constexpr (sizeof(T) == 2) x[i] = __uint_as_float(i & 1 ? q_raw[i / 2] & 0xffff0000u : q_raw[i / 2] << 16);
+                else x[i] = __uint_as_float(q_raw[i]);
+                top = fmaxf(top, fabsf(x[i]));
             }
 #pragma unroll
             for (int o = PER / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            // 2^(11 - e) with e the exponent of the largest (of a subnormal one: that of the smallest normal number)
-            int e = (int)(__float_as_uint(top) >> 23) - 127;
-            e = top == 0.f ? 11 : max(-126, min(127, e));
-            const float up = e > 11 - 127 ? ldexpf(1.f, 11 - e) : 0x1p127f;
-            if (sub == 0) q_scale[v] = logit_scale / up;
+            // 2^(11 - e) with e the exponent of the largest (at most 2^127: of tiny ones)
+            const int e = top == 0.f ? 11 : min(127, (int)(__float_as_uint(top) >> 23) - 127);
+            const float up = __uint_as_float((uint32_t)(127 + min(127, 11 - e)) << 23);
+            const int v = q_vec;
+            if (q_sub == 0) q_scale[v] = logit_scale / up;
             // lane (v % 8, lane_t) of tile v / 8 has numbers [D / 4 lane_t, D / 4 (lane_t + 1)), a step of the contraction four of them
 #pragma unroll
             for (int i = 0; i < EACH; i += 2) {
-                const int n = sub * EACH + i, lane_t = n / (D / 4), in = n % (D / 4);
+                const int n = q_sub * EACH + i, lane_t = n / (D / 4), in = n % (D / 4);
                 const int step = in / 4, pair = (in / 2) % 2;
                 uint32_t hi = half2_bits(x[i] * up, x[i + 1] * up);
 #pragma unroll
@@ -653,8 +695,7 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) att
         }
         __syncthreads();
         {
-            constexpr int PER = A4_THREADS / N, EACH = D / PER;
-            const int v = threadIdx.x / PER, sub = threadIdx.x % PER;
+            const int v = q_vec, sub = q_sub;
             float m = -INFINITY;
 #pragma unroll
             for (int i = 0; i < A4_WARPS; ++i) m = fmaxf(m, ml[(i * N + v) * 2]);
@@ -737,21 +778,22 @@ __global__ void __launch_bounds__(A4_MERGE_THREADS) attend4_merge_kernel(const _
     int64_t *prefix = reinterpret_cast<int64_t *>(smem);
     __shared__ int64_t part[A4_MERGE_THREADS / 32];
     __shared__ float top[ROWS][N], share[A4_MERGE_PARTS][N], den_of[A4_MERGE_PARTS][N], sums[SHARE][2][SHARE > 1 ? SLICE : 1];
-    // lengths and cu are older than the launch before this one, whose CTAs let this one start when they had waited for them
+    // lengths and cu are older than the launch before this one, whose CTAs let this one start when they had waited for them.  Its parts are
+    // not: every CTA waits for it, those without anything to join too, for what follows in the stream waits for this launch alone.
     const int64_t total = lay_line(a, N, prefix, part);
+    cudaGridDependencySynchronize();
     const int ctas = stretches(total, ctas_launched);
     const int b = blockIdx.x / (a.pool.kv_heads * max_groups), rest = blockIdx.x % (a.pool.kv_heads * max_groups);
     const int h = rest / max_groups, group = rest % max_groups;
-    const Request rq = request_at(a, b, N);
+    const Request rq = request_from(a, line_known(prefix, a.batch)[b], N);
     if (group >= rq.groups) return;
     const int64_t f0 = prefix[b] + (int64_t)(h * rq.groups + group) * rq.places, f1 = f0 + rq.places;
     // stretch c is [total c / ctas, total (c + 1) / ctas): the one that place f is in
-    const int64_t c0 = ((f0 + A4_START + 1) * ctas - 1) / total, c1 = (f1 * ctas - 1) / total;
+    const int64_t c0 = div_small((f0 + A4_START + 1) * ctas - 1, total), c1 = div_small(f1 * ctas - 1, total);
     if (c0 == c1) return;
-    cudaGridDependencySynchronize();
     const int count = (int)(c1 - c0 + 1);
     // its second segment at most: the first stretch may have begun with another problem
-    const int64_t slot0 = 2 * c0 + (total * c0 / ctas >= f0 ? 0 : 1);
+    const int64_t slot0 = 2 * c0 + (div_small(total * c0, ctas) >= f0 ? 0 : 1);
     auto slot = [&](int i) { return i == 0 ? slot0 : 2 * (c0 + i); };
     const float2 *ml = reinterpret_cast<const float2 *>(a.part + (int64_t)2 * ctas_launched * N * D);
     const int v = threadIdx.x % N, r = threadIdx.x / N;
@@ -835,9 +877,9 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
     using C = A4<D, NT, PARTS>;
     auto kern = attend4_kernel<T, D, NT, PARTS, LIST>;
     // CTAs per SM, asked once per device and size of the line (threads that meet here first find the same answer)
-    static std::atomic<int> known[64][2];
-    const bool big = a.batch > A4_FEW;
-    const int smem = C::total(big ? A4_MAX_BATCH : A4_FEW);
+    static std::atomic<int> known[64][3];
+    const int big = a.batch <= A4_FEW ? 0 : a.batch <= A4_SOME ? 1 : 2;
+    const int smem = C::total(big == 0 ? A4_FEW : big == 1 ? A4_SOME : A4_MAX_BATCH);
     int dev = 0;
     ELM_CUDA_TRY(cudaGetDevice(&dev));
     int per_sm = dev < 64 ? known[dev][big].load(std::memory_order_relaxed) : 0;
@@ -861,8 +903,8 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
             const int at = size == 2 ? 0 : size == 4 ? 1 : size == 8 ? 2 : 3;
             int clusters = dev < 64 ? resident[dev][at].load(std::memory_order_relaxed) : 0;
             if (clusters == 0) {
-                clusters = resident_clusters(kern, A4_THREADS, smem, size) + 1;       // (+ 1: 0 is not known yet)
-                ELM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::total(A4_MAX_BATCH)));
+                // (+ 1: 0 is not known yet.  Asked with the largest line: the question sets the kernel's limit)
+                clusters = resident_clusters(kern, A4_THREADS, C::total(A4_MAX_BATCH), size) + 1;
                 if (dev < 64) resident[dev][at].store(clusters, std::memory_order_relaxed);
             }
             if (problems > clusters - 1) continue;
@@ -894,7 +936,7 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
     const int slices = problems * FINE <= 2 * device_sm_count() ? FINE : problems * COARSE <= 2 * device_sm_count() ? COARSE : 1;
     auto join = slices == FINE ? attend4_merge_kernel<T, D, NT, FINE> : slices == COARSE ? attend4_merge_kernel<T, D, NT, COARSE> : attend4_merge_kernel<T, D, NT, 1>;
     const dim3 join_grid((unsigned)problems, (unsigned)slices);
-    ELM_CUDA_TRY(launch_after(join, join_grid, dim3(A4_MERGE_THREADS), (a.batch + 1) * 8, st, a, grid, max_groups));
+    ELM_CUDA_TRY(launch_after(join, join_grid, dim3(A4_MERGE_THREADS), line_bytes(a.batch), st, a, grid, max_groups));
     count_launches(2);
     return cuda_status(cudaGetLastError());
 }
@@ -1015,6 +1057,7 @@ extern "C" int elm_cache4_attend(const void *Q, const void *rows, const int32_t 
         a.qs[i] = zeros(p->q_stride) ? dense[i] : p->q_stride[i];
         a.os[i] = zeros(p->o_stride) ? dense[i] : p->o_stride[i];
     }
+    a.q_wide = (a.qs[0] * (int64_t)elt_bytes(p->dtype)) % 8 == 0 && (a.qs[1] * (int64_t)elt_bytes(p->dtype)) % 8 == 0 && (a.qs[2] * (int64_t)elt_bytes(p->dtype)) % 8 == 0;
     // rows of O that would be written twice
     if ((!cu && p->batch > 1 && a.os[0] == 0) || (p->q_heads > 1 && a.os[1] == 0) || ((cu ? p->n_tokens : p->n_q) > 1 && a.os[2] == 0)) return ELM_ERR_SHAPE;
     a.batch = p->batch;
