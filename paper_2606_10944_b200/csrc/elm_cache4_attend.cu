@@ -124,6 +124,13 @@ __device__ __forceinline__ uint32_t half2_rest(float lo, float hi, uint32_t roun
     const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&rounded));
     return half2_bits(lo - f.x, hi - f.y);
 }
+// bytes whose low halves are a's and whose high halves are b's, in one operation
+__device__ __forceinline__ uint32_t low_of_high_of(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, 0x0f0f0f0f, 0xe4;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
@@ -625,8 +632,8 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) att
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         const uint32_t r0 = vw[kb][x][0][w], r1 = vw[kb][x][1][w];
-                        codes8_to_half2((r0 & 0x0f0f0f0fu) | ((r1 * 16u) & 0xf0f0f0f0u), even[kb][x]);
-                        codes8_to_half2(((r0 >> 4) & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u), odd[kb][x]);
+                        codes8_to_half2(low_of_high_of(r0, r1 << 4), even[kb][x]);
+                        codes8_to_half2(low_of_high_of(r0 >> 4, r1), odd[kb][x]);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             even[kb][x][i] = hmul2_bits(even[kb][x][i], vs[kb][x]);
