@@ -1,7 +1,8 @@
 // New tokens into a pool of rows held in 4 bits (elm_cache4_append), and rows back (elm_cache4_read).
 //
 // Both are one pass over their rows.  Append reads 2 d numbers per token and KV head and writes a row (144 bytes at d = 128), besides the queries'
-// 2 d per query head; read the other way round.  HBM-bound in long calls, bound by the launch in a decode step.
+// 2 d per query head; read the other way round.  Bound by the launch in a decode step (16 tokens: 8 us the two), by HBM and the latency of a CTA's one round in
+// long ones (10 K tokens of 32 + 8 + 8 heads, 222 MB: 48 us = 4.6 TB/s; rows back, 178 MB written: 32 us = 5.6 TB/s).
 #include "elm_cache4.cuh"
 #include "elm_rope.cuh"
 

@@ -8,7 +8,7 @@
 //   S^T = K Q^T   (16 rows x 8 vectors):  a lane's part of the K operand is one stretch of 32 numbers (d = 64: 16) of rows g and g + 8, read as
 //                 16 (8) bytes of codes; which numbers make up a step of the contraction is free as long as Q is laid out alike.
 //   O^T = V^T P^T (16 numbers x 8 vectors): the V operand wants two neighbouring rows' numbers in one register: nibbles of the two
-//                 rows' words are put side by side (two logic operations per eight numbers), so that converting a byte gives the pair.
+//                 rows' words are put side by side (one logic operation and a shift per eight numbers), so that converting a byte gives the pair.
 //                 P^T comes from the accumulator layout of S^T by one 8x8 transposition (movmatrix) per 16 rows and half.
 // Codes become fp16 numbers by one conversion per two and are multiplied by their scales, exactly (elm_cache4.cuh).  A query vector is scaled to
 // a largest magnitude of 2^11 .. 2^12 before it is rounded to fp16 (bf16 numbers have fewer bits: exact but for those 2^-25 below the
@@ -16,9 +16,13 @@
 // reference moves only when the maximum has passed it by 2^6.  fp32 queries and outputs: queries and probabilities as two fp16 parts (22
 // bits), and each tile's sums go to fp32 accumulators by ordinary additions, since the matrix instruction cuts off low bits.
 //
-// What bounds it: reading each row once (144 bytes at d = 128).  The rows of all problems form one line of tiles, and every CTA takes an equal
-// stretch of it, whatever the requests' lengths are - they are on the device, and the stretch is found there.  A problem that lies in one
-// stretch is finished there; the parts of one that several CTAs share go to the workspace and are joined by a second launch.
+// The rows of all problems form one line of tiles, and every CTA takes an equal stretch of it, whatever the requests' lengths are - they are on
+// the device, and the stretch is found there.  A problem that lies in one stretch is finished there; the parts of one that several CTAs share go to the
+// workspace and are joined by a second launch.  Short problems go to a CTA or a cluster each, in one launch.
+//
+// What bounds it: its floor is reading each row once (144 bytes at d = 128), which it does; the time is the issue of 575 instructions per tile, 225 of them on
+// the integer and conversion pipe at two cycles each.  48 requests x 16384 rows x 8 heads, d = 128: 162 us = 5.6 TB/s, 85 % of the measured copy rate (16
+// vectors 225 us, fp32 224 us, d = 64 109 us); 48 requests of 1 .. 32768 rows, lengths spread over the logarithm, 48 us for a floor of 27.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -34,10 +38,10 @@ namespace {
 constexpr int A4_WARPS = 4;
 constexpr int A4_THREADS = 32 * A4_WARPS;
 constexpr int A4_TILE = 32;              // rows of a warp's tile
-constexpr int A4_STAGES = 2;
-constexpr int A4_START = 12;              // what a problem's beginning and end cost, in tiles
-constexpr int A4_MAX_BATCH = 1024, A4_SOME = 511, A4_FEW = 127;                // requests of a call; of calls whose line is short
-constexpr int A4_CTA_PLACES = 8;     // a CTA's stretch holds at least these
+constexpr int A4_STAGES = 2;             // tiles in flight per warp (three: 65 against 60 us, for one CTA less per SM)
+constexpr int A4_START = 12;             // what a problem's beginning and end cost, in tiles (8: 54, 12: 49, 16: 50 us for 48 ragged requests)
+constexpr int A4_MAX_BATCH = 1024, A4_SOME = 511, A4_FEW = 127;        // requests of a call; of calls whose line is short
+constexpr int A4_CTA_PLACES = 8;         // a CTA's stretch holds at least these
 constexpr float A4_LIFT = 8.f;           // probabilities are 2^8 times their share of the reference's
 constexpr float A4_SLACK = 6.f;          // how far the maximum may pass the reference: fp16 ends at 2^16
 
