@@ -457,6 +457,57 @@ def test_row_numbers_past_32_bits():
     assert np.array_equal(_np(k[0]), plain.unpack(plain.pack(_np(K), _np(K)), d)[0][[0, 2]].swapaxes(0, 1))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("H,rep,n_q,page", [(1, 2, 1, 16), (2, 4, 2, 32), (1, 3, 5, 128), (1, 20, 1, 1024)])
+def test_attend_stretches(dtype, d, H, rep, n_q, page):
+    """Tables of so many pages that the rows are one line cut into equal stretches: problems inside one, and over several, of every
+    form of the kernel, with rows that are on no page."""
+    r = np.random.default_rng(d + page)
+    lengths = [3000, 5, 0, 700, 4097, 64, 1]
+    table, n_pages = _tables(r, lengths, page, 9216 // page + 1)
+    small = _pool(r, 4, H, page, d)
+    pool = small[torch.as_tensor(r.integers(0, 4, n_pages))].contiguous()
+    table[0, 1], table[4, 4096 // page] = n_pages, -1
+    Q = torch.randn(len(lengths), H * rep, n_q, d, generator=torch.Generator().manual_seed(d)).to(DTYPES[dtype]).cuda()
+    got = elm.cache4_attend(Q, pool, _ints(table), length=_ints(lengths))
+    _check_lengths(pool, table, lengths, Q, got, None, page, d)
+
+
+@pytest.mark.parametrize("B,cap", [(33, 40), (130, 600), (600, 300), (1024, 9000)])
+def test_attend_many_requests(B, cap):
+    """As many requests as a call takes, most of them short, some without queries."""
+    r = np.random.default_rng(B)
+    d, H, rep, page = 64, 1, 2, 16
+    lengths = r.integers(0, 30, B)
+    lengths[B // 2], lengths[B - 1] = cap - 7, cap // 2
+    new = r.integers(0, 3, B)
+    table, n_pages = _tables(r, lengths, page, -(-cap // page))
+    pool = _pool(r, n_pages, H, page, d)
+    cu = np.concatenate([[0], np.cumsum(new)])
+    Q = torch.randn(int(cu[-1]), H * rep, d, generator=torch.Generator().manual_seed(B)).bfloat16().cuda()
+    wide = torch.full((int(cu[-1]), H * rep + 1, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    got = elm.cache4_attend(Q, pool, _ints(table), length=_ints(lengths), cu=_ints(cu), max_q=2, out=wide[:, 1:])
+    assert (wide[:, 0] == 9.0).all()
+    _check_lengths(pool, table, lengths, Q, got, cu, page, d)
+
+
+def test_append_of_many_heads():
+    """More heads than a block has threads for at once, of keys and of queries."""
+    r = np.random.default_rng(7)
+    T, H, Hq, d = 9, 70, 300, 128
+    x = torch.randn(T, Hq + 2 * H, d, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    Q, K, V = x[:, :Hq], x[:, Hq:Hq + H], x[:, Hq + H:]
+    for rotary in (128, 48):
+        rope = elm.Rope(rotary)
+        rows = torch.zeros(1, H, 16, 144, dtype=torch.uint8, device="cuda")
+        slots, pos = r.permutation(16)[:T], r.integers(0, 9999, T)
+        q = elm.cache4_append(rows, K, V, _ints(slots), rope=rope, positions=_ints(pos), Q=Q)
+        k = plain.rotate(K.float().cpu().numpy(), pos[:, None], rope.inv_freq, single=True)
+        assert np.array_equal(rows.cpu().numpy()[0][:, slots].swapaxes(0, 1), plain.pack(k.astype(np.float64), _np(V)))
+        assert torch.equal(q.cpu(), torch.as_tensor(plain.rotate(Q.float().cpu().numpy(), pos[:, None], rope.inv_freq, single=True)).bfloat16())
+
+
 # ------------------------------------------------------------------------------------------------
 # as they are used together
 # ------------------------------------------------------------------------------------------------
@@ -520,3 +571,37 @@ def test_coreset_of_a_stored_prompt():
     assert _by_tensor_cores(Q, pool, table, 256)
     many = elm.cache4_attend(Q, pool, table, idx=idx, w=w)
     assert torch.equal(many, elm.attend(Q, k, v, idx, w))     # the same kernel over the same bf16 rows
+
+
+def test_a_captured_decode_step():
+    """Plan, append and attention of a decode step in one graph, replayed as the requests grow over pages' ends: as the same calls made
+    one by one."""
+    B, H, rep, d, page, n_pages, max_pages = 5, 2, 4, 128, 16, 40, 8
+    rope = elm.Rope(d, layout="pairs")
+    x = torch.zeros(B, H * (rep + 2), d, dtype=torch.bfloat16, device="cuda")
+    Q, K, V = x[:, :H * rep], x[:, H * rep:H * (rep + 1)], x[:, H * (rep + 1):]
+    one = _ints([1] * B)
+
+    def state():
+        return dict(pool=torch.zeros(n_pages, H, page, 144, dtype=torch.uint8, device="cuda"), table=_ints(np.full((B, max_pages), -1)),
+                    length=_ints([0] * B), free=_ints(np.arange(n_pages)), count=_ints([n_pages]))
+
+    def step(s, out):
+        plan = elm.page_plan(s["table"], s["length"], one, s["free"], s["count"], page, B, length_out=s["length"], free_count_out=s["count"])
+        q = elm.cache4_append(s["pool"], K, V, plan.slots, rope=rope, positions=plan.positions, Q=Q)
+        return elm.cache4_attend(q, s["pool"], s["table"], length=s["length"], cu=plan.cu, max_q=1, out=out)
+
+    eager, kept = state(), state()
+    out, ref = torch.zeros_like(Q.contiguous()), torch.zeros_like(Q.contiguous())
+    step(state(), out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(kept, out)
+    g = torch.Generator().manual_seed(5)
+    for i in range(40):
+        x.copy_(torch.randn(x.shape, generator=g))
+        graph.replay()
+        step(eager, ref)
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref), i
+    assert kept["length"].tolist() == [40] * B and torch.equal(kept["pool"], eager["pool"]) and torch.equal(kept["table"], eager["table"])

@@ -32,7 +32,8 @@ def _check_rotation(got, x, pos, rope, layout, inverse, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("layout", ["halves", "pairs"])
 @pytest.mark.parametrize("B,H,n,d,rotary", [(1, 1, 1, 64, 64), (2, 3, 17, 128, 128), (1, 5, 33, 128, 64), (3, 2, 7, 64, 48), (2, 2, 9, 64, 6),
-                                            (1, 2, 5, 10, 2), (1, 1, 3, 256, 256), (2, 1, 11, 96, 96), (4, 32, 300, 128, 128)])
+                                            (1, 2, 5, 10, 2), (1, 1, 3, 256, 256), (2, 1, 11, 96, 96), (4, 32, 300, 128, 128), (1, 300, 3, 128, 128),
+                                            (2, 70, 2, 256, 32)])
 def test_rotation(dtype, layout, B, H, n, d, rotary):
     g = torch.Generator().manual_seed(B * 1000 + d + rotary)
     x = torch.randn(B, H, n, d, generator=g).to(DTYPES[dtype]).cuda()
@@ -103,6 +104,17 @@ def test_inverse_is_the_gradient():
     assert err <= (2 * (4 + 1) * 2.0 ** -24 * size) / (2 * h) + 5 * 2.0 ** -24 * size
 
 
+def test_first_position_of_any_size():
+    """A first position past 32 bits turns by the angle modulo a turn: a frequency of a quarter turn a position comes back every four."""
+    rope = elm.Rope(64)
+    rope._freq[:] = [np.pi / 2] * 32
+    x = torch.randn(1, 2, 8, 64, generator=torch.Generator().manual_seed(3)).cuda()
+    near, far = elm.rope(x, 1, rope), elm.rope(x, 2 ** 45 + 1, rope)
+    # (the frequency is off by 2^-53 of a radian: 2^-8 radians at 2^45)
+    assert (near - far).abs().max().item() <= 2 * x.abs().max().item() * 2.0 ** -7
+    assert torch.equal(elm.rope(x, -7, rope, inverse=True)[:, :, 0], elm.rope(x, 7, rope)[:, :, 0])
+
+
 def test_rope_other_stream_and_graph():
     rope = elm.Rope(128)
     x = torch.randn(1, 8, 64, 128, generator=torch.Generator().manual_seed(9)).cuda()
@@ -138,7 +150,7 @@ def _plan_both(table, length, n_new, free, count, page, T):
     return got, tab
 
 
-@pytest.mark.parametrize("B", [1, 2, 33, 1024, 1025, 5000])
+@pytest.mark.parametrize("B", [1, 2, 33, 1024, 1025, 5000, 65536])
 @pytest.mark.parametrize("page", [16, 256])
 @pytest.mark.parametrize("most,share", [(1, 1.0), (3, 0.5), (100, 0.7)])
 def test_plan(B, page, most, share):
