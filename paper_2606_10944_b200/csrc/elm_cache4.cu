@@ -74,16 +74,18 @@ __device__ __forceinline__ void rotate_group(const T *row, int first, int rotary
     }
 }
 
-template <typename T, int E, bool HALVES> __device__ __forceinline__ void turn_queries(const AppendArgs &a, const RopeTurns &turns, float *cs)
+template <typename T, int E, bool HALVES, bool WHOLE> __device__ __forceinline__ void turn_queries(const AppendArgs &a, const RopeTurns &turns, float *cs)
 {
     const int64_t t0 = (int64_t)blockIdx.x * a.query.tile;
-    rope_rows<T, E, HALVES>((const T *)a.q, (T *)a.q_out, a.query, turns, t0, min(a.query.tile, a.n_tokens - (int)t0), cs,
-                            [&](int64_t t, int64_t &from, int64_t &to, int64_t &pos) {
-                                from = t * a.qs[0];
-                                to = t * a.qos[0];
-                                pos = a.rotary ? a.positions[t] : 0;
-                                return (uint32_t)a.slots[t] < a.n_slots;
-                            });
+    const int count = min(a.query.tile, a.n_tokens - (int)t0);
+    auto token = [&](int64_t t, int64_t &from, int64_t &to, int64_t &pos) {
+        from = t * a.qs[0];
+        to = t * a.qos[0];
+        pos = a.rotary ? a.positions[t] : 0;
+        return (uint32_t)a.slots[t] < a.n_slots;
+    };
+    if constexpr (WHOLE) rope_rows<T, E, HALVES>((const T *)a.q, (T *)a.q_out, a.query, turns, t0, count, cs, token);
+    else rope_rows_any<T, E, HALVES>((const T *)a.q, (T *)a.q_out, a.query, turns, t0, count, cs, token);
 }
 
 // Queries are turned by the first CTAs as elm_rope does it; the others store rows, a thread two groups of 16 numbers: of a key that
@@ -96,7 +98,7 @@ __global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_const
     extern __shared__ __align__(16) float cs[];
     cudaGridDependencySynchronize();
     if ((int)blockIdx.x < a.q_ctas) {
-        turn_queries<T, E, HALVES>(a, turns, cs);
+        turn_queries<T, E, HALVES, true>(a, turns, cs);
         return;
     }
     // items: (token, head, key or value, pair of groups); a thread requests its first one's numbers before the cosines are formed
@@ -131,11 +133,10 @@ __global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_const
         }
     };
     request(threadIdx.x);
-    for (int i = threadIdx.x; i < count * pairs; i += APP_THREADS) {
-        const int ti = i / pairs, pi = i - ti * pairs;
-        *reinterpret_cast<float2 *>(cs + ti * row_cs + 2 * pi + 4 * (pi / 16)) = rope_cos_sin(a.positions[t0 + ti], turns.turn[pi], a.scale, a.scale);
-    }
-    __syncthreads();
+    __shared__ int64_t pos_of[APP_THREADS];
+    if (pairs > 0)
+        rope_table(turns, pairs, count, a.scale, a.scale, pos_of, [&](int ti, int64_t &at) { at = a.positions[t0 + ti]; return true; },
+                   [&](int ti, int pi) { return reinterpret_cast<float2 *>(cs + ti * row_cs + 2 * pi + 4 * (pi / 16)); });
     for (int i0 = threadIdx.x & ~31; i0 < total; i0 += APP_THREADS) {        // (whole warps stay together: lanes exchange scales)
         if (i0 >= APP_THREADS) request(i0 + (threadIdx.x & 31));
         uint32_t byte0 = 0, byte1 = 0;
@@ -199,8 +200,8 @@ __global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_const
 }
 
 // Rows whose numbers are not on 16-byte boundaries, or of which a part is rotated that is not whole groups on both sides: a thread takes one group of
-// 16 numbers of a key or a value.  WIDE: on 16-byte boundaries, halves of the rotated part included.
-template <typename T, int D, bool WIDE, bool HALVES>
+// 16 numbers of a key or a value.  WIDE: rows on 16-byte boundaries; WHOLE: halves of the rotated part, too (or neither).
+template <typename T, int D, bool WIDE, bool HALVES, bool WHOLE>
 __global__ void __launch_bounds__(APP_THREADS) append4_any_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTurns turns)
 {
     using R = Row4<D>;
@@ -208,18 +209,17 @@ __global__ void __launch_bounds__(APP_THREADS) append4_any_kernel(const __grid_c
     extern __shared__ __align__(16) float cs_floats[];
     cudaGridDependencySynchronize();
     if ((int)blockIdx.x < a.q_ctas) {
-        turn_queries<T, WIDE ? 16 / (int)sizeof(T) : 1, HALVES>(a, turns, cs_floats);
+        turn_queries<T, WIDE ? 16 / (int)sizeof(T) : 1, HALVES, WHOLE>(a, turns, cs_floats);
         return;
     }
     float2 *cs = reinterpret_cast<float2 *>(cs_floats);        // [tile][rotary / 2]
     const int pairs = a.rotary / 2;
     const int t0 = ((int)blockIdx.x - a.q_ctas) * a.tile;
     const int count = min(a.tile, a.n_tokens - t0);
-    for (int i = threadIdx.x; i < count * pairs; i += APP_THREADS) {
-        const int t = i / pairs;
-        cs[i] = rope_cos_sin(a.positions[t0 + t], turns.turn[i - t * pairs], a.scale, a.scale);
-    }
-    __syncthreads();
+    __shared__ int64_t pos_of[APP_THREADS];
+    if (pairs > 0)
+        rope_table(turns, pairs, count, a.scale, a.scale, pos_of, [&](int ti, int64_t &at) { at = a.positions[t0 + ti]; return true; },
+                   [&](int ti, int pi) { return cs + ti * pairs + pi; });
     const int total = count * a.kv_heads * 2 * G;
     for (int i0 = threadIdx.x & ~31; i0 < total; i0 += APP_THREADS) {        // (whole warps stay together: lanes exchange scales)
         const int i = i0 + (threadIdx.x & 31);
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(APP_THREADS) append4_any_kernel(const __grid_c
             const int first = (key ? j : j - G) * C4_GROUP;
             float x[C4_GROUP];
             load_group<T, WIDE>(src, first, x);
-            if (key) rotate_group<T, WIDE, HALVES>(src, first, a.rotary, cs + t * pairs, x);
+            if (key) rotate_group<T, WIDE && WHOLE, HALVES>(src, first, a.rotary, cs + t * pairs, x);
             uint2 codes;
             byte = quantise4(x, codes);
             const uint32_t page = slot >> a.page_shift, in_page = slot & ((1u << a.page_shift) - 1u);
@@ -326,17 +326,18 @@ template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &t
 {
     constexpr int E = 16 / (int)sizeof(T);
     const int sms = device_sm_count(), pairs = a.rotary / 2;
-    const bool wide = aligned && pairs % E == 0, groups = wide && a.rotary % 32 == 0;
+    const bool whole = pairs % E == 0, groups = aligned && a.rotary % 32 == 0;
     int64_t q_ctas = 0;
     size_t smem = 0;
     a.query = RopeShape{a.q_heads, a.rotary, 0, 0, 0, a.qs[1], a.qos[1], a.scale, a.scale};
     if (a.q_heads > 0) {
-        const int e = wide ? E : 1;
-        a.query.per_head = pairs / e + (a.q == a.q_out ? 0 : (D - a.rotary) / e);       // (in place, numbers that are not rotated stay)
+        const int e = aligned ? E : 1;
+        const bool any = aligned && !whole;
+        a.query.per_head = any ? D / E : pairs / e + (a.q == a.q_out ? 0 : (D - a.rotary) / e);      // (in place, numbers that are not rotated stay)
         if (a.query.per_head > 0) {
-            rope_share(a.query, a.n_tokens, sms);
+            rope_share(a.query, a.n_tokens, sms, any ? ROPE_ANY_AHEAD : ROPE_AHEAD);
             q_ctas = (a.n_tokens + a.query.tile - 1) / a.query.tile;
-            smem = (size_t)a.query.tile * (wide ? rope_cs_floats<E>(pairs) : rope_cs_floats<1>(pairs)) * sizeof(float);
+            smem = (size_t)a.query.tile * (aligned && whole ? rope_cs_floats<E>(pairs) : 2 * pairs) * sizeof(float);
         }
     }
     // an item a thread; fewer tokens per CTA where they would not fill the GPU
@@ -349,8 +350,9 @@ template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &t
     if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
     a.q_ctas = (int)q_ctas;
     auto kern = groups ? (halves ? append4_kernel<T, D, true> : append4_kernel<T, D, false>)
-                : wide ? (halves ? append4_any_kernel<T, D, true, true> : append4_any_kernel<T, D, true, false>)
-                       : (halves ? append4_any_kernel<T, D, false, true> : append4_any_kernel<T, D, false, false>);
+                : !aligned ? (halves ? append4_any_kernel<T, D, false, true, true> : append4_any_kernel<T, D, false, false, true>)
+                : whole ? (halves ? append4_any_kernel<T, D, true, true, true> : append4_any_kernel<T, D, true, false, true>)
+                        : (halves ? append4_any_kernel<T, D, true, true, false> : append4_any_kernel<T, D, true, false, false>);
     ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)ctas), dim3(APP_THREADS), smem, st, a, turns));
     count_launches(1);
     return cuda_status(cudaGetLastError());

@@ -20,31 +20,34 @@ struct RopeArgs {
     int64_t tokens;                      // batch * n_tokens
 };
 
-template <typename T, int E, bool HALVES>
+// WHOLE: the halves of a pair's chunk are whole chunks (or E is 1)
+template <typename T, int E, bool HALVES, bool WHOLE>
 __global__ void __launch_bounds__(ROPE_THREADS, 3) rope_kernel(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeTurns turns)
 {
     extern __shared__ __align__(16) float cs[];
     cudaGridDependencySynchronize();
     const int64_t t0 = (int64_t)blockIdx.x * a.shape.tile;
     const int count = (int)(a.tokens - t0 < a.shape.tile ? a.tokens - t0 : a.shape.tile);
-    rope_rows<T, E, HALVES>((const T *)a.x, (T *)a.out, a.shape, turns, t0, count, cs, [&](int64_t t, int64_t &from, int64_t &to, int64_t &pos) {
+    auto token = [&](int64_t t, int64_t &from, int64_t &to, int64_t &pos) {
         const uint32_t b = (uint32_t)t / (uint32_t)a.n_tokens, n = (uint32_t)t - b * (uint32_t)a.n_tokens;
         from = b * a.xs[0] + n * a.xs[1];
         to = b * a.os[0] + n * a.os[1];
         pos = a.positions ? (int64_t)a.positions[t] : a.first + n;
         return true;
-    });
+    };
+    if constexpr (WHOLE) rope_rows<T, E, HALVES>((const T *)a.x, (T *)a.out, a.shape, turns, t0, count, cs, token);
+    else rope_rows_any<T, E, HALVES>((const T *)a.x, (T *)a.out, a.shape, turns, t0, count, cs, token);
 }
 
-template <typename T, int E> int launch_rope(RopeArgs &a, int d, const RopeTurns &turns, bool halves, bool in_place, cudaStream_t st)
+template <typename T, int E, bool WHOLE> int launch_rope(RopeArgs &a, int d, const RopeTurns &turns, bool halves, bool in_place, cudaStream_t st)
 {
     const int pairs = a.shape.rotary / 2;
-    a.shape.per_head = pairs / E + (in_place ? 0 : (d - a.shape.rotary) / E);
-    rope_share(a.shape, a.tokens, device_sm_count());
+    a.shape.per_head = WHOLE ? pairs / E + (in_place ? 0 : (d - a.shape.rotary) / E) : d / E;
+    rope_share(a.shape, a.tokens, device_sm_count(), WHOLE ? ROPE_AHEAD : ROPE_ANY_AHEAD);
     const int64_t ctas = (a.tokens + a.shape.tile - 1) / a.shape.tile;
     if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
-    const size_t smem = (size_t)a.shape.tile * rope_cs_floats<E>(pairs) * sizeof(float);
-    auto kern = halves ? rope_kernel<T, E, true> : rope_kernel<T, E, false>;
+    const size_t smem = (size_t)a.shape.tile * (WHOLE ? rope_cs_floats<E>(pairs) : 2 * pairs) * sizeof(float);
+    auto kern = halves ? rope_kernel<T, E, true, WHOLE> : rope_kernel<T, E, false, WHOLE>;
     ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)ctas), dim3(ROPE_THREADS), smem, st, a, turns));
     count_launches(1);
     return cuda_status(cudaGetLastError());
@@ -98,12 +101,15 @@ extern "C" int elm_rope(const void *X, const int32_t *positions, int64_t first_p
     a.tokens = (int64_t)p->batch * p->n_tokens;
     cudaStream_t st = (cudaStream_t)stream;
     const bool halves = p->layout == ELM_ROPE_HALVES;
-    // 16 bytes at a time where every chunk starts on a 16-byte boundary and both numbers of a pair lie in whole chunks
+    // 16 bytes at a time where every row starts on a 16-byte boundary
     const int E = 16 / item;
-    const bool wide = !(((uintptr_t)X | (uintptr_t)out) & 15) && all % E == 0 && p->d % E == 0 && p->rotary_dim / 2 % E == 0;
+    const bool wide = !(((uintptr_t)X | (uintptr_t)out) & 15) && all % E == 0 && p->d % E == 0, whole = p->rotary_dim / 2 % E == 0;
+    typedef __nv_bfloat16 bf;
     if (p->dtype == ELM_BF16)
-        return wide ? launch_rope<__nv_bfloat16, 8>(a, p->d, turns, halves, in_place, st) : launch_rope<__nv_bfloat16, 1>(a, p->d, turns, halves, in_place, st);
-    return wide ? launch_rope<float, 4>(a, p->d, turns, halves, in_place, st) : launch_rope<float, 1>(a, p->d, turns, halves, in_place, st);
+        return !wide ? launch_rope<bf, 1, true>(a, p->d, turns, halves, in_place, st)
+               : whole ? launch_rope<bf, 8, true>(a, p->d, turns, halves, in_place, st) : launch_rope<bf, 8, false>(a, p->d, turns, halves, in_place, st);
+    return !wide ? launch_rope<float, 1, true>(a, p->d, turns, halves, in_place, st)
+           : whole ? launch_rope<float, 4, true>(a, p->d, turns, halves, in_place, st) : launch_rope<float, 4, false>(a, p->d, turns, halves, in_place, st);
 }
 
 extern "C" int elm_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double original, double low, double high,

@@ -32,13 +32,35 @@ inline bool rope_turns(const double *inv_freq, int pairs, RopeTurns &out)
 
 // (scale cos, scale sin) of a pair at a position, formed in fp64 and rounded once: two builds of a row's rotation that agree in
 // fp64 then agree in every bit of the fp32 products, and so in the 4-bit codes made of them, but for angles within 2^-28
-// of a rounding border.
+// of a rounding border.  The angle is the fraction of a turn less the nearest quarter, within pi / 4 either way; there the Taylor series up to the
+// 15th and 16th power end below 2^-53.  (18 operations in fp64; a general sine and cosine take several times as many instructions, which one head
+// of 378 K tokens waits for.)
 __device__ __forceinline__ float2 rope_cos_sin(int64_t position, uint64_t turn, double scale, double sin_scale)
 {
-    const int64_t frac = (int64_t)((uint64_t)position * turn);             // in [-1/2, 1/2) turns
-    double s, c;
-    sincospi((double)frac * 0x1p-63, &s, &c);
-    return make_float2((float)(c * scale), (float)(s * sin_scale));
+    const int64_t frac = (int64_t)((uint64_t)position * turn);             // in [-1/2, 1/2) turns, 64 bits
+    const int quarter = (int)((frac + ((int64_t)1 << 61)) >> 62);
+    const int64_t rest = (int64_t)((uint64_t)frac - ((uint64_t)(int64_t)quarter << 62));
+    const double x = (double)rest * (6.283185307179586476925286766559 * 0x1p-64), z = x * x;
+    double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;         // 1 / 15!, 1 / 16!
+    s = fma(s, z, 1.0 / 6227020800.0);
+    c = fma(c, z, -1.0 / 87178291200.0);
+    s = fma(s, z, -1.0 / 39916800.0);
+    c = fma(c, z, 1.0 / 479001600.0);
+    s = fma(s, z, 1.0 / 362880.0);
+    c = fma(c, z, -1.0 / 3628800.0);
+    s = fma(s, z, -1.0 / 5040.0);
+    c = fma(c, z, 1.0 / 40320.0);
+    s = fma(s, z, 1.0 / 120.0);
+    c = fma(c, z, -1.0 / 720.0);
+    s = fma(s, z, -1.0 / 6.0);
+    c = fma(c, z, 1.0 / 24.0);
+    s = fma(s * z, x, x);
+    c = fma(c, z, -0.5);
+    c = fma(c, z, 1.0);
+    // (c, s) turned by the quarters
+    const double cq = quarter & 1 ? s : c, sq = quarter & 1 ? c : s;
+    const double co = (quarter + 1) & 2 ? -cq : cq, si = quarter & 2 ? -sq : sq;
+    return make_float2((float)(co * scale), (float)(si * sin_scale));
 }
 
 // a' = a c - b s, b' = b c + a s; each product and sum rounded by itself (no fma), so that the result does not depend on how
@@ -95,13 +117,47 @@ template <typename T, int E> struct Chunk {
     }
 };
 
+// Cosines and sines of `count` tokens at place(token, pair) of shared memory, by the whole CTA.  A thread keeps its pair; with many tokens their
+// positions are looked up once beforehand (one head of 378 K tokens: 210 -> 143 us; with few, that and its barrier cost 4 %).  `position` gives false for a
+// token that is passed over.
+constexpr int ROPE_THREADS = 256;
+template <typename Position, typename Place>
+__device__ __forceinline__ void rope_table(const RopeTurns &turns, int pairs, int count, double scale, double sin_scale, int64_t *pos_of, Position position, Place place)
+{
+    const int shift = pairs > 1 ? 32 - __clz(pairs - 1) : 0;               // pairs rounded up to a power of two: no division in the loop
+    const int p = threadIdx.x & ((1 << shift) - 1);
+    if ((count << shift) <= 2 * ROPE_THREADS) {
+        // a token or two to a thread
+        for (int t = threadIdx.x >> shift; t < count; t += ROPE_THREADS >> shift) {
+            int64_t at;
+            if (p < pairs && position(t, at)) *place(t, p) = rope_cos_sin(at, turns.turn[p], scale, sin_scale);
+        }
+        __syncthreads();
+        return;
+    }
+    constexpr int64_t NONE = INT64_MIN;
+    for (int t = threadIdx.x; t < count; t += ROPE_THREADS) {
+        int64_t at;
+        pos_of[t] = position(t, at) ? at : NONE;
+    }
+    __syncthreads();
+    if (p < pairs) {
+        const uint64_t turn = turns.turn[p];
+#pragma unroll 2
+        for (int t = threadIdx.x >> shift; t < count; t += ROPE_THREADS >> shift) {
+            const int64_t at = pos_of[t];
+            if (at != NONE) *place(t, p) = rope_cos_sin(at, turn, scale, sin_scale);
+        }
+    }
+    __syncthreads();
+}
+
 // A CTA's share of a rotation: `tile` tokens, each by heads_at_once x per_head threads.  Cosines and sines are formed first; a thread then keeps
 // those of its chunk in registers from head to head (read again from shared memory for each head, they took more of the load/store unit than the
 // numbers themselves).  Its first heads are requested before the cosines are formed; CTAs that go on to further tokens with the same cosine table
 // were slower (32 heads x 32768 tokens: 92 us; two rounds of tokens 104, four 112), for their loads then wait for their stores.
 //   HALVES: item j < rotary / 2 / E holds numbers [E j, E j + E) and their partners rotary / 2 further on.  PAIRS: item j holds 2 E numbers side by
 //   side.  Items from there on copy E numbers (none where out is x).
-constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_AHEAD = 4;            // heads of a thread that are requested together
 struct RopeShape {
     int32_t heads, rotary, per_head, heads_at_once, tile;
@@ -110,10 +166,10 @@ struct RopeShape {
     uint64_t zero = 0x8000000080000000ull;       // (-0, -0), as an argument: of a constant the compiler would make use
 };
 // `tokens`: how many there are; per_head <= ROPE_THREADS
-inline void rope_share(RopeShape &r, int64_t tokens, int sms)
+inline void rope_share(RopeShape &r, int64_t tokens, int sms, int ahead = ROPE_AHEAD)
 {
-    // a thread takes ROPE_AHEAD heads, fewer where the tokens would not fill the GPU
-    int each = ROPE_AHEAD;
+    // a thread takes `ahead` heads, fewer where the tokens would not fill the GPU
+    int each = ahead;
     while (each > 1 && tokens * r.per_head * ((r.heads + each - 1) / each) < (int64_t)2 * sms * ROPE_THREADS) each >>= 1;
     r.heads_at_once = (r.heads + each - 1) / each;
     if (r.heads_at_once * r.per_head > ROPE_THREADS) r.heads_at_once = ROPE_THREADS / r.per_head;
@@ -181,14 +237,13 @@ __device__ __forceinline__ void rope_rows(const T *x, T *out, const RopeShape &r
     };
     request(h0);
     const uint64_t zero = r.zero;
-    for (int i = threadIdx.x; i < count * pairs; i += ROPE_THREADS) {
-        const int ti = i / pairs, p = i - ti * pairs;
-        int64_t f, g, at;
-        if (!token(t0 + ti, f, g, at)) continue;
-        const float2 c = rope_cos_sin(at, turns.turn[p], r.scale, r.sin_scale);
-        *reinterpret_cast<float2 *>(cs + ti * row_cs + 2 * p + (E >= 4 ? 4 * (p / E) : 0)) = c;
-    }
-    __syncthreads();
+    __shared__ int64_t pos_of[ROPE_THREADS];
+    rope_table(turns, pairs, count, r.scale, r.sin_scale, pos_of,
+               [&](int ti, int64_t &at) {
+                   int64_t f, g;
+                   return token(t0 + ti, f, g, at);
+               },
+               [&](int ti, int p) { return reinterpret_cast<float2 *>(cs + ti * row_cs + 2 * p + (E >= 4 ? 4 * (p / E) : 0)); });
     if (!mine) return;
     // HALVES: cosines and sines of pairs 2 i, 2 i + 1 side by side; PAIRS: (c, c) and (-s, s) of pair i
     uint64_t cc[E > 1 ? E : 1], ss[E > 1 ? E : 1];
@@ -245,6 +300,65 @@ __device__ __forceinline__ void rope_rows(const T *x, T *out, const RopeShape &r
                 w[k].store(dst + partner);
             }
             u[k].store(dst);
+        }
+    }
+}
+
+// The same where rows are on 16-byte boundaries and the halves of a pair's chunk are not: a thread loads and stores whole chunks of E numbers and
+// reads the partners of its numbers one by one, from L1.  per_head is d / E.  Between the reads and the stores of a round the CTA waits, for out may
+// be x and a row is several threads'.
+constexpr int ROPE_ANY_AHEAD = 2;
+template <typename T, int E, bool HALVES, typename Token>
+__device__ __forceinline__ void rope_rows_any(const T *x, T *out, const RopeShape &r, const RopeTurns &turns, int64_t t0, int count, float *cs, Token token)
+{
+    const int pairs = r.rotary / 2;
+    const int per_token = r.heads_at_once * r.per_head;
+    const int t = threadIdx.x / per_token, rest = threadIdx.x - t * per_token, h0 = rest / r.per_head, first = (rest - h0 * r.per_head) * E;
+    int64_t from = 0, to = 0, pos = 0;
+    const bool mine = t < count && token(t0 + t, from, to, pos);
+    __shared__ int64_t pos_of[ROPE_THREADS];
+    rope_table(turns, pairs, count, r.scale, r.sin_scale, pos_of,
+               [&](int ti, int64_t &at) {
+                   int64_t f, g;
+                   return token(t0 + ti, f, g, at);
+               },
+               [&](int ti, int p) { return reinterpret_cast<float2 *>(cs) + ti * pairs + p; });
+    const float2 *c = reinterpret_cast<const float2 *>(cs) + t * pairs;
+    for (int round = 0; round < r.heads; round += ROPE_ANY_AHEAD * r.heads_at_once) {
+        Chunk<T, E> u[ROPE_ANY_AHEAD], w[ROPE_ANY_AHEAD];
+#pragma unroll
+        for (int k = 0; k < ROPE_ANY_AHEAD; ++k) {
+            const int h = round + h0 + k * r.heads_at_once;
+            if (!mine || h >= r.heads) continue;
+            const T *row = x + from + h * r.x_head;
+            u[k].load(row + first);
+            if constexpr (HALVES) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int j = first + e;
+                    w[k].v[e] = j < r.rotary ? load_as<float>(row, j < pairs ? j + pairs : j - pairs) : 0.f;
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < ROPE_ANY_AHEAD; ++k) {
+            const int h = round + h0 + k * r.heads_at_once;
+            if (!mine || h >= r.heads) continue;
+#pragma unroll
+            for (int e = 0; e < E; e += HALVES ? 1 : 2) {
+                const int j = first + e;
+                if (j >= r.rotary) continue;
+                if constexpr (HALVES) {
+                    const bool lower = j < pairs;
+                    float a = lower ? u[k].v[e] : w[k].v[e], b = lower ? w[k].v[e] : u[k].v[e];
+                    rope_turn(a, b, c[lower ? j : j - pairs]);
+                    u[k].v[e] = lower ? a : b;
+                } else {
+                    rope_turn(u[k].v[e], u[k].v[e + 1], c[j / 2]);
+                }
+            }
+            u[k].store(out + to + h * r.out_head + first);
         }
     }
 }
