@@ -329,11 +329,11 @@ template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &t
     const bool whole = pairs % E == 0, groups = aligned && a.rotary % 32 == 0;
     int64_t q_ctas = 0;
     size_t smem = 0;
-    a.query = RopeShape{a.q_heads, a.rotary, 0, 0, 0, a.qs[1], a.qos[1], a.scale, a.scale};
+    a.query = RopeShape{a.q_heads, a.rotary, 0, 0, 0, 1, a.qs[1], a.qos[1], a.scale, a.scale};
     if (a.q_heads > 0) {
-        const int e = aligned ? E : 1;
         const bool any = aligned && !whole;
-        a.query.per_head = any ? D / E : pairs / e + (a.q == a.q_out ? 0 : (D - a.rotary) / e);      // (in place, numbers that are not rotated stay)
+        if (any) a.query.per_head = D / E;
+        else rope_items(a.query, aligned ? E : 1, a.q == a.q_out ? 0 : D - a.rotary);        // (in place, numbers that are not rotated stay)
         if (a.query.per_head > 0) {
             rope_share(a.query, a.n_tokens, sms, any ? ROPE_ANY_AHEAD : ROPE_AHEAD);
             q_ctas = (a.n_tokens + a.query.tile - 1) / a.query.tile;

@@ -42,7 +42,8 @@ __global__ void __launch_bounds__(ROPE_THREADS, 3) rope_kernel(const __grid_cons
 template <typename T, int E, bool WHOLE> int launch_rope(RopeArgs &a, int d, const RopeTurns &turns, bool halves, bool in_place, cudaStream_t st)
 {
     const int pairs = a.shape.rotary / 2;
-    a.shape.per_head = WHOLE ? pairs / E + (in_place ? 0 : (d - a.shape.rotary) / E) : d / E;
+    if (WHOLE) rope_items(a.shape, E, in_place ? 0 : d - a.shape.rotary);
+    else a.shape.per_head = d / E;
     rope_share(a.shape, a.tokens, device_sm_count(), WHOLE ? ROPE_AHEAD : ROPE_ANY_AHEAD);
     const int64_t ctas = (a.tokens + a.shape.tile - 1) / a.shape.tile;
     if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
@@ -96,7 +97,7 @@ extern "C" int elm_rope(const void *X, const int32_t *positions, int64_t first_p
         a.xs[i] = xs[2 * i];
         a.os[i] = os[2 * i];
     }
-    a.shape = RopeShape{p->heads, p->rotary_dim, 0, 0, 0, xs[1], os[1], p->scale, p->inverse ? -p->scale : p->scale};
+    a.shape = RopeShape{p->heads, p->rotary_dim, 0, 0, 0, 1, xs[1], os[1], p->scale, p->inverse ? -p->scale : p->scale};
     a.n_tokens = p->n_tokens;
     a.tokens = (int64_t)p->batch * p->n_tokens;
     cudaStream_t st = (cudaStream_t)stream;

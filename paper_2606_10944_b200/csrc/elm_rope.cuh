@@ -157,14 +157,21 @@ __device__ __forceinline__ void rope_table(const RopeTurns &turns, int pairs, in
 // numbers themselves).  Its first heads are requested before the cosines are formed; CTAs that go on to further tokens with the same cosine table
 // were slower (32 heads x 32768 tokens: 92 us; two rounds of tokens 104, four 112), for their loads then wait for their stores.
 //   HALVES: item j < rotary / 2 / E holds numbers [E j, E j + E) and their partners rotary / 2 further on.  PAIRS: item j holds 2 E numbers side by
-//   side.  Items from there on copy E numbers (none where out is x).
+//   side.  Items from there on copy E or, where their number is even, 2 E numbers (none where out is x).
 constexpr int ROPE_AHEAD = 4;            // heads of a thread that are requested together
 struct RopeShape {
     int32_t heads, rotary, per_head, heads_at_once, tile;
+    int32_t copy;                        // chunks that an item copies: 1 or 2
     int64_t x_head, out_head;            // strides
     double scale, sin_scale;
     uint64_t zero = 0x8000000080000000ull;       // (-0, -0), as an argument: of a constant the compiler would make use
 };
+// items of a head whose halves are whole chunks of E numbers; `copied`: numbers that are copied
+inline void rope_items(RopeShape &r, int E, int copied)
+{
+    r.copy = copied / E % 2 == 0 ? 2 : 1;
+    r.per_head = r.rotary / 2 / E + copied / E / r.copy;
+}
 // `tokens`: how many there are; per_head <= ROPE_THREADS
 inline void rope_share(RopeShape &r, int64_t tokens, int sms, int ahead = ROPE_AHEAD)
 {
@@ -219,7 +226,8 @@ __device__ __forceinline__ void rope_rows(const T *x, T *out, const RopeShape &r
     const int per_token = r.heads_at_once * r.per_head;
     const int t = threadIdx.x / per_token, rest = threadIdx.x - t * per_token, h0 = rest / r.per_head, j = rest - h0 * r.per_head;
     const bool turn = j < turn_items;
-    const int o = turn ? (HALVES ? j * E : 2 * j * E) : r.rotary + (j - turn_items) * E, partner = HALVES ? pairs : E;
+    const int o = turn ? (HALVES ? j * E : 2 * j * E) : r.rotary + (j - turn_items) * r.copy * E, partner = HALVES && turn ? pairs : E;
+    const bool two = turn || r.copy == 2;
     Raw<T, E> u[ROPE_AHEAD], w[ROPE_AHEAD];
     int64_t from = 0, to = 0, pos = 0;
     const bool mine = t < count && token(t0 + t, from, to, pos);
@@ -230,7 +238,7 @@ __device__ __forceinline__ void rope_rows(const T *x, T *out, const RopeShape &r
         for (int k = 0; k < ROPE_AHEAD; ++k) {
             if (mine && first + k * r.heads_at_once < r.heads) {
                 u[k].load(src);
-                if (turn) w[k].load(src + partner);
+                if (two) w[k].load(src + partner);
             }
             src += step;
         }
@@ -297,8 +305,8 @@ __device__ __forceinline__ void rope_rows(const T *x, T *out, const RopeShape &r
                         z.set(e % (E / 2), sm100::add2(sm100::fma2(ab, cc[e], zero), sm100::fma2(sm100::pack2(b, a), ss[e], zero)));
                     }
                 }
-                w[k].store(dst + partner);
             }
+            if (two) w[k].store(dst + partner);
             u[k].store(dst);
         }
     }
