@@ -337,7 +337,7 @@ template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &t
         if (a.query.per_head > 0) {
             rope_share(a.query, a.n_tokens, sms, any ? ROPE_ANY_AHEAD : ROPE_AHEAD);
             q_ctas = (a.n_tokens + a.query.tile - 1) / a.query.tile;
-            smem = (size_t)a.query.tile * (aligned && whole ? rope_cs_floats<E>(pairs) : 2 * pairs) * sizeof(float);
+            smem = (size_t)a.query.tile * (any ? 2 * rope_any_places(pairs) : aligned ? rope_cs_floats<E>(pairs) : rope_cs_floats<1>(pairs)) * sizeof(float);
         }
     }
     // an item a thread; fewer tokens per CTA where they would not fill the GPU

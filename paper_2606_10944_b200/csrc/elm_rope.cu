@@ -47,7 +47,7 @@ template <typename T, int E, bool WHOLE> int launch_rope(RopeArgs &a, int d, con
     rope_share(a.shape, a.tokens, device_sm_count(), WHOLE ? ROPE_AHEAD : ROPE_ANY_AHEAD);
     const int64_t ctas = (a.tokens + a.shape.tile - 1) / a.shape.tile;
     if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
-    const size_t smem = (size_t)a.shape.tile * (WHOLE ? rope_cs_floats<E>(pairs) : 2 * pairs) * sizeof(float);
+    const size_t smem = (size_t)a.shape.tile * (WHOLE ? rope_cs_floats<E>(pairs) : 2 * rope_any_places(pairs)) * sizeof(float);
     auto kern = halves ? rope_kernel<T, E, true, WHOLE> : rope_kernel<T, E, false, WHOLE>;
     ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)ctas), dim3(ROPE_THREADS), smem, st, a, turns));
     count_launches(1);

@@ -316,6 +316,9 @@ __device__ __forceinline__ void rope_rows(const T *x, T *out, const RopeShape &r
 // reads the partners of its numbers one by one, from L1.  per_head is d / E.  Between the reads and the stores of a round the CTA waits, for out may
 // be x and a row is several threads'.
 constexpr int ROPE_ANY_AHEAD = 2;
+// where a pair's cosine and sine stand: chunks of eight pairs are 72 bytes apart, so that neighbouring threads' reads meet no bank twice
+__host__ __device__ constexpr int rope_any_place(int pair) { return pair + (pair >> 3); }
+__host__ __device__ constexpr int rope_any_places(int pairs) { return pairs + (pairs >> 3) + 1; }
 template <typename T, int E, bool HALVES, typename Token>
 __device__ __forceinline__ void rope_rows_any(const T *x, T *out, const RopeShape &r, const RopeTurns &turns, int64_t t0, int count, float *cs, Token token)
 {
@@ -324,16 +327,8 @@ __device__ __forceinline__ void rope_rows_any(const T *x, T *out, const RopeShap
     const int t = threadIdx.x / per_token, rest = threadIdx.x - t * per_token, h0 = rest / r.per_head, first = (rest - h0 * r.per_head) * E;
     int64_t from = 0, to = 0, pos = 0;
     const bool mine = t < count && token(t0 + t, from, to, pos);
-    __shared__ int64_t pos_of[ROPE_THREADS];
-    rope_table(turns, pairs, count, r.scale, r.sin_scale, pos_of,
-               [&](int ti, int64_t &at) {
-                   int64_t f, g;
-                   return token(t0 + ti, f, g, at);
-               },
-               [&](int ti, int p) { return reinterpret_cast<float2 *>(cs) + ti * pairs + p; });
-    const float2 *c = reinterpret_cast<const float2 *>(cs) + t * pairs;
-    for (int round = 0; round < r.heads; round += ROPE_ANY_AHEAD * r.heads_at_once) {
-        Chunk<T, E> u[ROPE_ANY_AHEAD], w[ROPE_ANY_AHEAD];
+    Chunk<T, E> u[ROPE_ANY_AHEAD], w[ROPE_ANY_AHEAD];
+    auto request = [&](int round) {
 #pragma unroll
         for (int k = 0; k < ROPE_ANY_AHEAD; ++k) {
             const int h = round + h0 + k * r.heads_at_once;
@@ -341,13 +336,35 @@ __device__ __forceinline__ void rope_rows_any(const T *x, T *out, const RopeShap
             const T *row = x + from + h * r.x_head;
             u[k].load(row + first);
             if constexpr (HALVES) {
+                if (sizeof(T) == 2 && (pairs & 1) == 0) {        // two at a time: both on one side
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int j = first + e;
-                    w[k].v[e] = j < r.rotary ? load_as<float>(row, j < pairs ? j + pairs : j - pairs) : 0.f;
+                    for (int e = 0; e < E; e += 2) {
+                        const int j = first + e;
+                        const uint32_t two = j < r.rotary ? *reinterpret_cast<const uint32_t *>(row + (j < pairs ? j + pairs : j - pairs)) : 0u;
+                        w[k].v[e] = __uint_as_float(two << 16);
+                        w[k].v[e + 1] = __uint_as_float(two & 0xffff0000u);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const int j = first + e;
+                        w[k].v[e] = j < r.rotary ? load_as<float>(row, j < pairs ? j + pairs : j - pairs) : 0.f;
+                    }
                 }
             }
         }
+    };
+    request(0);
+    __shared__ int64_t pos_of[ROPE_THREADS];
+    rope_table(turns, pairs, count, r.scale, r.sin_scale, pos_of,
+               [&](int ti, int64_t &at) {
+                   int64_t f, g;
+                   return token(t0 + ti, f, g, at);
+               },
+               [&](int ti, int p) { return reinterpret_cast<float2 *>(cs) + ti * rope_any_places(pairs) + rope_any_place(p); });
+    const float2 *c = reinterpret_cast<const float2 *>(cs) + t * rope_any_places(pairs);
+    for (int round = 0; round < r.heads; round += ROPE_ANY_AHEAD * r.heads_at_once) {
+        if (round) request(round);
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < ROPE_ANY_AHEAD; ++k) {
@@ -360,10 +377,10 @@ __device__ __forceinline__ void rope_rows_any(const T *x, T *out, const RopeShap
                 if constexpr (HALVES) {
                     const bool lower = j < pairs;
                     float a = lower ? u[k].v[e] : w[k].v[e], b = lower ? w[k].v[e] : u[k].v[e];
-                    rope_turn(a, b, c[lower ? j : j - pairs]);
+                    rope_turn(a, b, c[rope_any_place(lower ? j : j - pairs)]);
                     u[k].v[e] = lower ? a : b;
                 } else {
-                    rope_turn(u[k].v[e], u[k].v[e + 1], c[j / 2]);
+                    rope_turn(u[k].v[e], u[k].v[e + 1], c[rope_any_place(j / 2)]);
                 }
             }
             u[k].store(out + to + h * r.out_head + first);
