@@ -57,15 +57,8 @@ __device__ __forceinline__ uint32_t scale4_half_bits(uint32_t byte) { return byt
 __device__ __forceinline__ uint32_t scale4_half2(uint32_t low, uint32_t high) { return low * 0x80u + high * 0x800000u; }
 __device__ __forceinline__ uint32_t scale4_half2(uint32_t both) { return both * 0x00800080u; }
 
-// Two codes (a byte, the lower half first) as two fp16 numbers.  Codes are at most 6, scales at most 10240 with 4 bits, products have 6
-// bits and are at most 61440: fp16 holds them exactly, and so does bf16.
-__device__ __forceinline__ uint32_t codes2_to_half2(uint32_t byte)
-{
-    uint32_t out;
-    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\t}" : "=r"(out) : "r"(byte));
-    return out;
-}
-// all four bytes of a word
+// The eight codes of a word as pairs of fp16 numbers, the lower half of each byte first.  Codes are at most 6, scales at most 10240 with 4 bits, products
+// have 6 bits and are at most 61440: fp16 holds them exactly, and so does bf16.
 __device__ __forceinline__ void codes8_to_half2(uint32_t word, uint32_t (&out)[4])
 {
     asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"

@@ -774,7 +774,9 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) att
     }
 }
 
-// Joins the parts of a problem (request, KV head, group) that stretches share, in their order; a CTA per problem and slice of its numbers.
+// Joins the parts of a problem (request, KV head, group) that stretches share, in their order; a CTA per problem and slice of its numbers, or, with
+// more problems than stretches, a CTA per stretch but the first, which takes the problem that its stretch goes on with if no stretch before it did
+// (so that a bound of the queries that is far too high costs nothing).
 // With few problems of many parts a problem's numbers are cut into slices, so that more CTAs read (8 problems of 32768 rows, 74 parts each:
 // one CTA per problem took longer than the attention itself).  Each number's parts are dealt to SHARE threads.
 constexpr int A4_MERGE_THREADS = 256;
@@ -794,14 +796,28 @@ __global__ void __launch_bounds__(A4_MERGE_THREADS) attend4_merge_kernel(const _
     const int64_t total = lay_line(a, N, prefix, part);
     cudaGridDependencySynchronize();
     const int ctas = stretches(total, ctas_launched);
-    const int b = blockIdx.x / (a.pool.kv_heads * max_groups), rest = blockIdx.x % (a.pool.kv_heads * max_groups);
-    const int h = rest / max_groups, group = rest % max_groups;
-    const Request rq = request_from(a, line_known(prefix, a.batch)[b], N);
-    if (group >= rq.groups) return;
+    int b, h, group;
+    Request rq;
+    if (max_groups > 0) {
+        b = blockIdx.x / (a.pool.kv_heads * max_groups);
+        const int rest = blockIdx.x % (a.pool.kv_heads * max_groups);
+        h = rest / max_groups;
+        group = rest % max_groups;
+        rq = request_from(a, line_known(prefix, a.batch)[b], N);
+        if (group >= rq.groups) return;
+    } else {
+        if ((int)blockIdx.x + 1 >= ctas) return;
+        const int64_t f = div_small(total * (blockIdx.x + 1), ctas);
+        b = request_of(prefix, a.batch, f);
+        rq = request_from(a, line_known(prefix, a.batch)[b], N);
+        const int problem = (int)div_small(f - prefix[b], rq.places);
+        h = problem / rq.groups;
+        group = problem - h * rq.groups;
+    }
     const int64_t f0 = prefix[b] + (int64_t)(h * rq.groups + group) * rq.places, f1 = f0 + rq.places;
     // stretch c is [total c / ctas, total (c + 1) / ctas): the one that place f is in
     const int64_t c0 = div_small((f0 + A4_START + 1) * ctas - 1, total), c1 = div_small(f1 * ctas - 1, total);
-    if (c0 == c1) return;
+    if (c0 == c1 || (max_groups == 0 && c0 != (int64_t)blockIdx.x)) return;
     const int count = (int)(c1 - c0 + 1);
     // its second segment at most: the first stretch may have begun with another problem
     const int64_t slot0 = 2 * c0 + (div_small(total * c0, ctas) >= f0 ? 0 : 1);
@@ -909,6 +925,8 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
     const int tiles = (a.n_kv + A4_TILE - 1) / A4_TILE;
     for (int size = 1; size <= 16; size *= 2) {
         if (tiles > size * A4_WARPS * (size == 16 ? 4 : 2)) continue;
+        // (the queries of a request may be far fewer than their bound: then CTAs by the bound would be mostly idle ones)
+        if (size == 1 && a.cu && max_groups > 1 && problems > 32 * (int64_t)device_sm_count()) continue;
         if (size > 1) {
             static std::atomic<int> resident[64][5];
             const int at = size == 2 ? 0 : size == 4 ? 1 : size == 8 ? 2 : 3;
@@ -942,13 +960,16 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
     const int64_t places = problems * (A4_START + (a.n_kv + A4_TILE - 1) / A4_TILE);
     const int grid = stretches(places, per_sm * device_sm_count());
     ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)grid), dim3(A4_THREADS), smem, st, a));
+    count_launches(1);
     // slices of 32 or 128 numbers where the problems alone are few
     constexpr int FINE = C::N * D / 32, COARSE = C::N * D / 128;
     const int slices = problems * FINE <= 2 * device_sm_count() ? FINE : problems * COARSE <= 2 * device_sm_count() ? COARSE : 1;
     auto join = slices == FINE ? attend4_merge_kernel<T, D, NT, FINE> : slices == COARSE ? attend4_merge_kernel<T, D, NT, COARSE> : attend4_merge_kernel<T, D, NT, 1>;
-    const dim3 join_grid((unsigned)problems, (unsigned)slices);
-    ELM_CUDA_TRY(launch_after(join, join_grid, dim3(A4_MERGE_THREADS), line_bytes(a.batch), st, a, grid, max_groups));
-    count_launches(2);
+    const bool by_stretch = slices == 1 && problems >= grid;
+    if (by_stretch && grid == 1) return cuda_status(cudaGetLastError());       // (one stretch: nothing to join)
+    const dim3 join_grid(by_stretch ? (unsigned)(grid - 1) : (unsigned)problems, (unsigned)slices);
+    ELM_CUDA_TRY(launch_after(join, join_grid, dim3(A4_MERGE_THREADS), line_bytes(a.batch), st, a, grid, by_stretch ? 0 : max_groups));
+    count_launches(1);
     return cuda_status(cudaGetLastError());
 }
 template <typename T, int D, int NT, int PARTS> int launch_attend4(const Attend4Args &a, cudaStream_t st)

@@ -492,6 +492,28 @@ def test_attend_many_requests(B, cap):
     _check_lengths(pool, table, lengths, Q, got, cu, page, d)
 
 
+@pytest.mark.parametrize("n_kv", [200, 6000])
+def test_attend_far_bound_of_queries(n_kv):
+    """max_q far above the tokens that requests have."""
+    r = np.random.default_rng(3)
+    d, H, rep, page, B = 128, 4, 4, 16, 40
+    lengths = r.integers(1, 190, B)
+    if n_kv > 200:
+        lengths[7] = 5600
+    new = r.integers(0, 6, B)
+    table, n_pages = _tables(r, lengths, page, -(-n_kv // page))
+    small = _pool(r, 8, H, page, d)
+    pool = small[torch.as_tensor(r.integers(0, 8, n_pages))].contiguous()
+    cu = np.concatenate([[0], np.cumsum(new)])
+    Q = torch.randn(int(cu[-1]), H * rep, d, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    args = dict(length=_ints(lengths), cu=_ints(cu))
+    ref = elm.cache4_attend(Q, pool, _ints(table), max_q=5, **args)
+    _check_lengths(pool, table, lengths, Q, ref, cu, page, d)
+    for max_q in (50, 3000):
+        got = elm.cache4_attend(Q, pool, _ints(table), max_q=max_q, **args)
+        _check_lengths(pool, table, lengths, Q, got, cu, page, d)
+
+
 def test_append_of_many_heads():
     """More heads than a block has threads for at once, of keys and of queries."""
     r = np.random.default_rng(7)
