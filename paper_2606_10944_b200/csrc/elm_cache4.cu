@@ -2,7 +2,7 @@
 //
 // Both are one pass over their rows.  Append reads 2 d numbers per token and KV head and writes a row (144 bytes at d = 128), besides the queries'
 // 2 d per query head; read the other way round.  Bound by the launch in a decode step (16 tokens: 8 us the two), by HBM and the latency of a CTA's one round in
-// long ones (10 K tokens of 32 + 8 + 8 heads, 222 MB: 48 us = 4.6 TB/s; rows back, 178 MB written: 32 us = 5.6 TB/s).
+// long ones (10 K tokens of 32 + 8 + 8 heads, 222 MB: 46 us = 4.8 TB/s; rows back, 178 MB written: 32 us = 5.6 TB/s).
 #include "elm_cache4.cuh"
 #include "elm_rope.cuh"
 
@@ -90,8 +90,9 @@ template <typename T, int E, bool HALVES, bool WHOLE> __device__ __forceinline__
 
 // Queries are turned by the first CTAs as elm_rope does it; the others store rows, a thread two groups of 16 numbers: of a key that
 // is rotated in halves both halves of its pairs.  The groups of a row are neighbouring lanes, so that its codes leave in one piece.
+// (four CTAs per SM with bf16 numbers: 80 -> 78 us for prompts stored and read back)
 template <typename T, int D, bool HALVES>
-__global__ void __launch_bounds__(APP_THREADS) append4_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTurns turns)
+__global__ void __launch_bounds__(APP_THREADS, sizeof(T) == 2 ? 4 : 2) append4_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTurns turns)
 {
     using R = Row4<D>;
     constexpr int G = R::GROUPS, E = 16 / (int)sizeof(T), HALF = G / 2;
