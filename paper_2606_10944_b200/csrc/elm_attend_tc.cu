@@ -210,17 +210,12 @@ __global__ void __launch_bounds__(256) gather4_tc_kernel(Pool4 pool, const int32
         w_mine = w[at];
         if (w_mine > 0.f) row_mine = pool_row(pool, b, h, idx[at]);
     }
-    // a problem none of whose entries is there: its columns must not be hidden all (the attention takes the distance to the largest logit,
-    // and -1e30 is so large that its own rounding would be one); with logits and values of 0 its outputs are 0
-    float hidden = -1e30f;
-    if (!__syncthreads_or(row_mine != NO_ROW)) {
-        int any = 0;
-        for (int e0 = 0; e0 < n_core && !any; e0 += 256) {
-            const int64_t at = (int64_t)p * n_core + e0 + threadIdx.x;
-            any = __syncthreads_or(e0 + (int)threadIdx.x < n_core && w[at] > 0.f && pool_row(pool, b, h, idx[at]) != NO_ROW);
-        }
-        if (!any) hidden = 0.f;
-    }
+    // Here all 128 columns of a block may be hidden, and that block may be the first one seen by a row, so that the row's reference is
+    // the hidden columns' own logit and their probabilities are 2^(logit x scale - reference).  The attention forms that
+    // distance by an fma, exact product less rounded product: of -1e30 it is the product's rounding, 4e21 or 8e21, and the probabilities are infinite.
+    // A power of two has no rounding, in bf16 or in the product: they are 1, their values 0, and the next block with an entry
+    // that is there scales what they left in the denominator by 2^(-2^99 scale) = 0.  Without any such block the output is 0 / n_pad.
+    constexpr float hidden = -0x1p99f;
     const int chunk = lane & 15;                               // eight numbers of the key (lanes 0 .. 15), of the value
 #pragma unroll 4
     for (int i = 0; i < GATHER_COLS / 8; ++i) {

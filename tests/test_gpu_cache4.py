@@ -627,3 +627,49 @@ def test_a_captured_decode_step():
         torch.cuda.synchronize()
         assert torch.equal(out, ref), i
     assert kept["length"].tolist() == [40] * B and torch.equal(kept["pool"], eager["pool"]) and torch.equal(kept["table"], eager["table"])
+
+
+def _check_many(pool, table, idx, w, Q, got, page, d):
+    """Lists met by many queries: probabilities 2^-8 (numerator; the denominator sums them unrounded), their exponentials partly by a cubic:
+    1e-4 twice."""
+    B, H = idx.shape[:2]
+    rep = Q.shape[1] // H
+    for b in range(B):
+        for h in range(H):
+            i = idx[b, h]
+            there = np.array([0 <= x < table.shape[1] * page and 0 <= table[b, x // page] < pool.shape[0] for x in i]) & (w[b, h] > 0)
+            k, v = _rows_of(pool, table, b, h, i[there], page, d)
+            q = _np(Q[b, h * rep:(h + 1) * rep]).reshape(-1, d)
+            o, size, reach, most = plain.attend(q, k, v, np.ones((len(q), len(k)), bool), np.log(w[b, h][there]))
+            out = _np(got[b, h * rep:(h + 1) * rep]).reshape(-1, d)
+            assert np.isfinite(out).all(), (b, h)
+            assert (np.abs(out - o) <= plain.attend_bound(o, size, reach, most, torch.bfloat16, len(i)) + (2.0 ** -8 + 2e-4) * size).all(), (b, h)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("hidden", [(0, 127), (0, 128), (0, 200), (0, 256), (0, 499), (128, 256), (200, 500), (1, 500)])
+def test_attend_list_of_many_queries_blocks_not_seen(d, hidden):
+    """Whole blocks of 128 entries that are not seen, the first among them: by weights of 0 and below, by negative numbers, by pages that are
+    none; one problem of which everything is seen, with one weight, beside them."""
+    r = np.random.default_rng(d + hidden[1])
+    B, H, rep, page, n, n_q, n_core = 3, 2, 2, 64, 900, 701, 500
+    table, n_pages = _tables(r, [n] * B, page, 16)
+    pool = _pool(r, n_pages, H, page, d)
+    idx, w = _list(r, B, H, n, n_core)
+    a, e = hidden
+    table[1, 2] = n_pages + 1
+    idx[1][idx[1] // page == 2] = 5
+    w[0, 0, a:e] = 0.0
+    w[0, 1, a:e] = -1.0
+    idx[1, 0, a:e] = -1
+    idx[1, 1, a:e] = 2 * page + np.arange(e - a) % page
+    w[2, 0] = 2.0 ** -9
+    w[2, 1] = np.nan
+    w[2, 1, e - 1] = 1.0
+    Q = torch.randn(B, H * rep, n_q, d, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    assert _by_tensor_cores(Q, pool, table, n_core)
+    args = dict(idx=_ints(idx), w=torch.as_tensor(w, dtype=torch.float32).cuda())
+    got = elm.cache4_attend(Q, pool, _ints(table), **args)
+    _check_many(pool, table, idx, w, Q, got, page, d)
+    few = elm.cache4_attend(Q[:, :, :2].contiguous(), pool, _ints(table), **args)
+    _check_list(pool, table, idx, w, Q[:, :, :2].contiguous(), few, page, d)
