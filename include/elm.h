@@ -356,7 +356,9 @@ int elm_cache4_row_bytes(int32_t d, size_t *bytes);
  *   length_out   [batch] rows after the step; may be `length` itself
  *   free_count_out  [1]; may be `free_count` itself.  free is not written: entries past the new count are the taken ones
  *   cu_out       [batch + 1] first place of each request's tokens, and their total (negative n_new count as 0)
- *   position_out, slot_out  [max_tokens] of every place; -1 where there is no token or its request did not fit
+ *   position_out, slot_out  [max_tokens] of every place; -1 where there is no token or its request did not fit; slot_out is -1 too where
+ *                the token's page is negative or so large a number that its rows' would pass 2^31 - 1 (the pool's size is not known here:
+ *                elm_cache4_append passes over slots behind its end)
  * batch 1 .. 65536; max_tokens >= 0; free_count above the list's capacity n_free counts as n_free. */
 typedef struct elm_page_params {
     int32_t batch, max_pages, page_rows, max_tokens, n_free;
@@ -366,7 +368,7 @@ int elm_page_plan(int32_t *table, const int32_t *length, const int32_t *n_new, c
                   int32_t *cu_out, int32_t *position_out, int32_t *slot_out, void *stream);
 /* Gives the pages of every request with done[b] != 0 back: they are put at the end of free (in order of request and page), its table
  * entries become -1, its length 0.  *free_count is updated; pages for which free (capacity n_free) has no room, and table entries that
- * are negative, are dropped.  max_tokens is not used. */
+ * are negative or whose rows' numbers would pass 2^31 - 1, are dropped.  max_tokens is not used. */
 int elm_page_release(int32_t *table, int32_t *length, const int32_t *done, int32_t *free, int32_t *free_count,
                      const elm_page_params *params, void *stream);
 

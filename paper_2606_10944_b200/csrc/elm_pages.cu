@@ -49,6 +49,9 @@ struct PlanArgs {
     int32_t batch, max_pages, page_shift, max_tokens, n_free;
 };
 
+// whether some pool can have the page: one whose rows' numbers pass 2^31 - 1 is none (modulo 2^32 they would be another page's)
+__device__ __forceinline__ bool is_page(int32_t page, int page_shift) { return (uint32_t)page < (0x7fffffffu >> page_shift); }
+
 // last b in [lo, hi] with cu[b] <= t (cu[lo] <= t)
 template <typename Cu> __device__ __forceinline__ int request_of(const Cu &cu, int lo, int hi, int t)
 {
@@ -66,7 +69,7 @@ __device__ __forceinline__ void fill_place(const PlanArgs &a, int t, int b, int 
     if (start >= 0) {
         pos = start + (t - cu_b);
         const int32_t page = a.table[(int64_t)b * a.max_pages + (pos >> a.page_shift)];
-        if (page >= 0) slot = (int32_t)(((uint32_t)page << a.page_shift) + (uint32_t)(pos & ((1 << a.page_shift) - 1)));
+        if (is_page(page, a.page_shift)) slot = (page << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
     }
     a.position_out[t] = pos;
     a.slot_out[t] = slot;
@@ -231,7 +234,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) page_release_kernel(const __grid
                     else lo = mid + 1;
                 }
                 int32_t *entry = a.table + (int64_t)(b0 + lo) * a.max_pages + (k - (lo ? upto[lo - 1] : 0));
-                page = *entry;
+                page = is_page(*entry, a.page_shift) ? *entry : -1;
                 *entry = -1;
             }
             int64_t back;

@@ -237,3 +237,34 @@ def test_plan_captured():
     torch.cuda.synchronize()
     assert n.tolist() == [33, 33, 33] and c.item() == 3 and r.positions.tolist() == [32, 32, 32]
     assert sorted(t.cpu()[:, :3].reshape(-1).tolist()) == list(range(3, 12))
+
+
+@pytest.mark.parametrize("tokens", [40, 5000])                # one launch, two launches
+@pytest.mark.parametrize("page", [16, 32, 1024])
+def test_pages_that_no_pool_holds(page, tokens):
+    """Page numbers whose rows' numbers would pass 2^31 - 1, in a table and among the free ones: their tokens are in no slot, instead of in that of
+    another page modulo 2^32; given back, they are dropped.  The last page that a pool can hold is one."""
+    most = (2 ** 31 - 1) // page                              # pages of the largest pool
+    bad = [most, most + 1, 2 ** 32 // page // 2, 2 ** 31 - 1]
+    if page == 32:
+        bad += [1 << 27, (1 << 27) + 1]
+    table = np.full((len(bad) + 2, 9), -1)
+    table[:len(bad), 0] = bad
+    table[len(bad), 0] = most - 1
+    length = np.array([5] * len(bad) + [7, 0])
+    n_new = np.array([3] * len(bad) + [2, 3])
+    free = np.array([4, bad[-1], bad[0]])                     # (the last request's page)
+    t, n, f, c = _ints(table), _ints(length), _ints(free), _ints([3])
+    got = elm.page_plan(t, n, _ints(n_new), f, c, page, tokens, length_out=n, free_count_out=c)
+    slots = got.slots.tolist()
+    at = 3 * len(bad)
+    assert slots[:at] == [-1] * at and got.positions[:at].tolist() == [5, 6, 7] * len(bad)
+    assert slots[at:at + 2] == [(most - 1) * page + 7, (most - 1) * page + 8] and set(slots[at + 2:]) == {-1}
+    assert c.item() == 2
+    # nothing is stored through them
+    pool = torch.full((4, 1, page, 80), 0xa5, dtype=torch.uint8, device="cuda")
+    x = torch.randn(tokens, 1, 64, generator=torch.Generator().manual_seed(1)).cuda()
+    elm.cache4_append(pool, x, x, got.slots)
+    assert (pool == 0xa5).all()
+    elm.page_release(t, n, _ints([1] * len(table)), f, c, page)
+    assert c.item() == 3 and f.tolist() == [4, bad[-1], most - 1] and (t == -1).all() and (n == 0).all()
