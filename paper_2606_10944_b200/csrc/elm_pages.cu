@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(FILL_THREADS) page_fill_kernel(const __grid_co
     __shared__ int32_t cu[EACH + 1], start[EACH];
     cudaGridDependencySynchronize();
     const int t0 = blockIdx.x * EACH;
-    const int t1 = min(t0 + EACH, a.max_tokens) - 1;
+    const int t1 = min(EACH, a.max_tokens - t0) + (t0 - 1);     // (t0 + EACH may be 2^31)
     const int total = a.cu_out[a.batch];
     // the requests of the CTA's first and last place, each found by a warp, 32 ways at a time
     if (threadIdx.x < 64) {
@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(FILL_THREADS) page_fill_kernel(const __grid_co
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < FILL_EACH; ++i) {
-        const int t = t0 + i * FILL_THREADS + threadIdx.x;
-        if (t > t1) continue;
+        const int at = i * FILL_THREADS + threadIdx.x, t = t0 + at;
+        if (at > t1 - t0) continue;
         if (t >= total) {
             a.position_out[t] = -1;
             a.slot_out[t] = -1;

@@ -268,3 +268,18 @@ def test_pages_that_no_pool_holds(page, tokens):
     assert (pool == 0xa5).all()
     elm.page_release(t, n, _ints([1] * len(table)), f, c, page)
     assert c.item() == 3 and f.tolist() == [4, bad[-1], most - 1] and (t == -1).all() and (n == 0).all()
+
+
+def test_plan_of_as_many_places_as_there_can_be():
+    """A step of 2^31 - 1 places (17 GB of results): tokens in the first of them, all others marked."""
+    most = 2 ** 31 - 1
+    t, n = _ints(np.full((2, 400), -1)), _ints([3, 0])
+    t[0, 0] = 7
+    got = elm.page_plan(t, n, _ints([4, 6000]), _ints(np.arange(400) + 10), _ints([400]), 16, most)
+    assert got.cu.tolist() == [0, 4, 6004] and got.start.tolist() == [3, 0] and got.free_count.item() == 400 - 375
+    assert got.positions[:6004].tolist() == [3, 4, 5, 6] + list(range(6000))
+    assert got.slots[:4].tolist() == [7 * 16 + i for i in (3, 4, 5, 6)]
+    table = t[1].tolist()
+    assert got.slots[4:6004].tolist() == [table[i // 16] * 16 + i % 16 for i in range(6000)]
+    for x in (got.positions, got.slots):
+        assert all(bool((part == -1).all()) for part in x[6004:].split(1 << 28))
