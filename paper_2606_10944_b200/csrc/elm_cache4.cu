@@ -337,7 +337,7 @@ template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &t
         else rope_items(a.query, aligned ? E : 1, a.q == a.q_out ? 0 : D - a.rotary);        // (in place, numbers that are not rotated stay)
         if (a.query.per_head > 0) {
             rope_share(a.query, a.n_tokens, sms, any ? ROPE_ANY_AHEAD : ROPE_AHEAD);
-            q_ctas = (a.n_tokens + a.query.tile - 1) / a.query.tile;
+            q_ctas = ((int64_t)a.n_tokens + a.query.tile - 1) / a.query.tile;
             smem = (size_t)a.query.tile * (any ? 2 * rope_any_places(pairs) : aligned ? rope_cs_floats<E>(pairs) : rope_cs_floats<1>(pairs)) * sizeof(float);
         }
     }
@@ -347,7 +347,7 @@ template <typename T, int D> int launch_append(AppendArgs &a, const RopeTurns &t
     if (a.tile < 1) a.tile = 1;
     const size_t rows_smem = (size_t)a.tile * (groups ? rope_cs_floats<16>(pairs) : 2 * pairs) * sizeof(float);
     if (rows_smem > smem) smem = rows_smem;
-    const int64_t ctas = q_ctas + (a.n_tokens + a.tile - 1) / a.tile;
+    const int64_t ctas = q_ctas + ((int64_t)a.n_tokens + a.tile - 1) / a.tile;
     if (ctas > 0x7fffffff) return ELM_ERR_SHAPE;
     a.q_ctas = (int)q_ctas;
     auto kern = groups ? (halves ? append4_kernel<T, D, true> : append4_kernel<T, D, false>)

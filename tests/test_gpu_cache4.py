@@ -673,3 +673,17 @@ def test_attend_list_of_many_queries_blocks_not_seen(d, hidden):
     _check_many(pool, table, idx, w, Q, got, page, d)
     few = elm.cache4_attend(Q[:, :, :2].contiguous(), pool, _ints(table), **args)
     _check_list(pool, table, idx, w, Q[:, :, :2].contiguous(), few, page, d)
+
+
+def test_append_of_as_many_tokens_as_there_can_be():
+    """2^31 - 1 places (8.6 GB of slots) of which four are tokens, keys and values one row for all: the four are stored."""
+    T, d, page = 2 ** 31 - 1, 64, 16
+    k = torch.randn(1, 1, d, generator=torch.Generator().manual_seed(1)).cuda()
+    rows = torch.full((2, 1, page, 80), 0xa5, dtype=torch.uint8, device="cuda")
+    slots = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    for t, slot in ((0, 3), (1 << 30, 17), (T - 64, 9), (T - 1, 31)):
+        slots[t] = slot
+    elm.cache4_append(rows, k.expand(T, 1, d), k.expand(T, 1, d), slots)
+    want = np.full((2 * page, 80), 0xa5, np.uint8)
+    want[[3, 17, 9, 31]] = plain.pack(_np(k), _np(k))[0, 0]
+    assert np.array_equal(rows.cpu().numpy()[:, 0].reshape(-1, 80), want)
