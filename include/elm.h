@@ -412,6 +412,7 @@ int elm_cache4_read(const void *rows, const int32_t *table, const int32_t *lengt
  *   length [batch]       the request's rows 0 .. length - 1 (the exact attention of Eq. (unmaskedatt); with `causal` of its last n_q tokens,
  *                        Eq. (def:att)).  Requests with different numbers of queries: cu [batch + 1] on the device (that of
  *                        elm_page_plan), request b has the tokens cu[b] .. cu[b + 1] - 1 of Q and O; batch strides are not used.
+ *                        Of a request with more than n_q tokens, or with some behind n_tokens, the first are answered, as among all of them.
  *   idx, w [batch][kv_heads][n_kv]  a weighted list of the request's rows, as elm_attend takes it; every query sees all of it.
  * Rows that are not there, and list entries whose weight is not above 0, are not seen, whatever they hold; a query that sees
  * nothing gets zeros.  Tokens of O outside cu, and those of requests without queries, are left as they were.  O may be Q with the

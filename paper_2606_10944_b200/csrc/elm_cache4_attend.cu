@@ -66,6 +66,7 @@ struct Attend4Args {
 // what is known of a request, and what follows from it
 struct Request {
     int32_t rows, tokens, first_token, groups, tiles, places;
+    int32_t seen0;                       // rows that the first token sees, of all the request's tokens (some may be cut off): <= 0 is none
 };
 __device__ __forceinline__ Request request_from(const Attend4Args &a, int4 known, int n_vec)
 {
@@ -73,6 +74,7 @@ __device__ __forceinline__ Request request_from(const Attend4Args &a, int4 known
     r.rows = known.x;
     r.tokens = known.y;
     r.first_token = known.z;
+    r.seen0 = r.rows - known.w + 1;
     r.groups = (r.tokens * a.rep + n_vec - 1) / n_vec;
     r.tiles = max(1, (r.rows + A4_TILE - 1) / A4_TILE);
     r.places = A4_START + r.tiles;
@@ -80,12 +82,12 @@ __device__ __forceinline__ Request request_from(const Attend4Args &a, int4 known
 }
 __device__ __forceinline__ int4 look_at_request(const Attend4Args &a, int b)
 {
-    int4 r = make_int4(a.n_kv, a.n_q, 0, 0);
+    int4 r = make_int4(a.n_kv, a.n_q, 0, a.n_q);
     if (!a.idx) r.x = a.length[b];
     if (a.cu) {
         r.z = a.cu[b];
-        r.y = a.cu[b + 1] - r.z;
-        // only tokens that Q has
+        r.w = r.y = a.cu[b + 1] - r.z;
+        // only tokens that Q has; which rows those see goes by all of them
         if (r.z < 0 || r.y < 0) r.y = 0;
         else if ((int64_t)r.z + r.y > a.n_tokens) r.y = max(0, a.n_tokens - r.z);
         r.y = min(r.y, a.n_q);
@@ -281,10 +283,10 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) att
         const bool whole = tile0 == 0 && tile1 == rq.tiles;
         const int vec0 = group * N;                              // vector v of the group is token (vec0 + v) / rep, head h rep + (vec0 + v) % rep
         const int vectors = min(N, rq.tokens * a.rep - vec0);
-        // rows a vector sees: the last token all of them, the one before it one less
+        // rows a vector sees: the last token of the request all of them, the one before it one less
         const bool tail = !LIST && a.causal;
-        const int last_seen = tail ? rq.rows - rq.tokens + 1 + (vec0 + vectors - 1) / a.rep : rq.rows;
-        const int first_seen = tail ? rq.rows - rq.tokens + 1 + vec0 / a.rep : rq.rows;
+        const int last_seen = tail ? rq.seen0 + (vec0 + vectors - 1) / a.rep : rq.rows;
+        const int first_seen = tail ? rq.seen0 + vec0 / a.rep : rq.rows;
         const int tile_end = min(tile1, (last_seen + A4_TILE - 1) / A4_TILE);
 
         // ---- the queries are asked for first: vector q_vec by PER threads ----
@@ -432,7 +434,7 @@ __global__ void __launch_bounds__(A4_THREADS, NT == 1 && PARTS == 1 ? 4 : 3) att
                 ref[n][x] = limit[n][x] = -INFINITY;
                 lift[n][x] = 0.f;
                 qs[n][x] = q_scale[v];
-                seen[n][x] = tail ? rq.rows - rq.tokens + 1 + (vec0 + v) / a.rep : rq.rows;
+                seen[n][x] = tail ? rq.seen0 + (vec0 + v) / a.rep : rq.rows;
             }
 #pragma unroll
             for (int i = 0; i < KS; ++i)

@@ -687,3 +687,31 @@ def test_append_of_as_many_tokens_as_there_can_be():
     want = np.full((2 * page, 80), 0xa5, np.uint8)
     want[[3, 17, 9, 31]] = plain.pack(_np(k), _np(k))[0, 0]
     assert np.array_equal(rows.cpu().numpy()[:, 0].reshape(-1, 80), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("held,max_q", [(10, 33), (100, 5), (7, 5), (41, 33)])
+def test_attend_tokens_cut_off(dtype, held, max_q):
+    """Requests of which Q holds the first tokens only, or that have more than max_q: those see the rows that they would see among all
+    of them."""
+    r = np.random.default_rng(5)
+    d, H, rep, page = 128, 2, 4, 32
+    lengths, new = [7, 2500, 64, 33, 40, 1], [3, 9, 0, 33, 4, 1]
+    table, n_pages = _tables(r, lengths, page, 100)
+    pool = _pool(r, n_pages, H, page, d)
+    cu = np.concatenate([[0], np.cumsum(new)])
+    Q = torch.randn(held, H * rep, d, generator=torch.Generator().manual_seed(6)).to(DTYPES[dtype]).cuda()
+    for causal in (True, False):
+        out = torch.full_like(Q, 5.0)
+        elm.cache4_attend(Q, pool, _ints(table), length=_ints(lengths), cu=_ints(cu), max_q=max_q, causal=causal, out=out)
+        written = np.zeros(held, bool)
+        for b, n in enumerate(lengths):
+            for j in range(min(new[b], max_q, max(0, held - cu[b]))):
+                t = cu[b] + j
+                written[t] = True
+                for h in range(H):
+                    k, v = _rows_of(pool, table, b, h, np.arange(n), page, d)
+                    upto = n - new[b] + 1 + j if causal else n
+                    ref = plain.attend(_np(Q[t, h * rep:(h + 1) * rep]), k, v, np.broadcast_to(np.arange(n) < upto, (rep, n)))
+                    _check(out[t, h * rep:(h + 1) * rep], *ref, Q.dtype, n, (b, h, j))
+        assert (out[torch.as_tensor(~written)] == 5.0).all()
