@@ -420,7 +420,8 @@ int elm_cache4_read(const void *rows, const int32_t *table, const int32_t *lengt
  * length: what its tokens of O hold afterwards means nothing.)
  * dtype is that of Q and O: ELM_BF16 (probabilities rounded to fp16 for P V) or ELM_F32 (queries and probabilities as two fp16
  * parts); logits, maxima, denominators and accumulators are fp32 either way.  batch <= 1024.
- * bf16 lists met by many queries take the tensor-core kernel of elm_attend over a gathered bf16 copy (dense Q and O only).
+ * bf16 lists met by many queries take the tensor-core kernel of elm_attend over a gathered bf16 copy (dense Q and O only), as long as
+ * the workspace that holds the copy is not above 8 GiB.
  * workspace: at least the bytes of elm_cache4_attend_workspace_bytes, 256-byte aligned, scratch; two calls that overlap in time (two
  * graphs on two streams among them) need separate ones.  Q, O and rows are 16-byte aligned.
  * elm_cache4_attend_status: as elm_attend_status.

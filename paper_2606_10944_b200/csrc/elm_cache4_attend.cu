@@ -996,23 +996,6 @@ int check(const elm_cache4_params *p, bool list, int &shift, int64_t &n_kv)
     return ELM_OK;
 }
 
-// Lists met by so many queries that the tensor-core kernel of elm_attend over a gathered copy, 256 queries of a head at a time, is the faster
-// way.  Both forms' times in us, as they were measured (lists of 1024, 2048 and 16384 entries, 4 to 256 queries of 8 to 256 heads, d = 128):
-//   here     9 + 0.9 (A4_START + tiles) per CTA slot and problem     8 heads x 4, 2048 entries: 128 queries 45 (44), 256 queries 71 (78)
-//   there   14 + 2.2 per block of 128 entries and wave of items      the same: 49 (49), 51 (49)
-// With 2 or 3 queries the first form is 4 to 6 times as fast, with thousands the second.
-bool by_tensor_cores(const elm_cache4_params *p, bool list)
-{
-    if (!list || p->dtype != ELM_BF16 || !zeros(p->q_stride) || !zeros(p->o_stride)) return false;
-    const int sms = device_sm_count();
-    const int64_t rep = p->q_heads / p->kv_heads, vectors = rep * p->n_q <= 8 ? 8 : 16;
-    const double problems = (double)p->batch * p->kv_heads * ((rep * p->n_q + vectors - 1) / vectors);
-    const double here = 9.0 + 0.9 * problems * (A4_START + (p->n_kv + A4_TILE - 1) / A4_TILE) / (4.0 * sms);
-    const int64_t items = (int64_t)p->batch * p->q_heads * ((p->n_q + 255) / 256), waves = (items + sms - 1) / sms;
-    const double there = 14.0 + 2.2 * (double)waves * ((p->n_kv + 127) / 128);
-    return there < here;
-}
-
 elm_params as_attend(const elm_cache4_params *p)
 {
     elm_params e = {};
@@ -1026,6 +1009,27 @@ elm_params as_attend(const elm_cache4_params *p)
     e.precision = ELM_PREC_FP32;
     e.delta = 0.5;
     return e;
+}
+
+// Lists met by so many queries that the tensor-core kernel of elm_attend over a gathered copy, 256 queries of a head at a time, is the faster
+// way.  Both forms' times in us, as they were measured (lists of 1024, 2048 and 16384 entries, 4 to 256 queries of 8 to 256 heads, d = 128):
+//   here     9 + 0.9 (A4_START + tiles) per CTA slot and problem     8 heads x 4, 2048 entries: 128 queries 45 (44), 256 queries 71 (78)
+//   there   14 + 2.2 per block of 128 entries and wave of items      the same: 49 (49), 51 (49)
+// With 2 or 3 queries the first form is 4 to 6 times as fast, with thousands the second.  Its gathered copy has to fit the workspace: 552 bytes an
+// entry and KV head (d = 64: 296), a twentieth of the GPU's memory at most (15 M entries), which also keeps clear of what that kernel can count.
+constexpr size_t A4_MAX_COPY = (size_t)8 << 30;
+bool by_tensor_cores(const elm_cache4_params *p, bool list)
+{
+    if (!list || p->dtype != ELM_BF16 || !zeros(p->q_stride) || !zeros(p->o_stride)) return false;
+    const int sms = device_sm_count();
+    const int64_t rep = p->q_heads / p->kv_heads, vectors = rep * p->n_q <= 8 ? 8 : 16;
+    const double problems = (double)p->batch * p->kv_heads * ((rep * p->n_q + vectors - 1) / vectors);
+    const double here = 9.0 + 0.9 * problems * (A4_START + (p->n_kv + A4_TILE - 1) / A4_TILE) / (4.0 * sms);
+    const int64_t items = (int64_t)p->batch * p->q_heads * ((p->n_q + 255) / 256), waves = (items + sms - 1) / sms;
+    const double there = 14.0 + 2.2 * (double)waves * ((p->n_kv + 127) / 128);
+    if (there >= here) return false;
+    const elm_params e = as_attend(p);
+    return attend_layout(&e, p->n_kv).total <= A4_MAX_COPY;
 }
 
 size_t workspace_of(const elm_cache4_params *p, bool list)

@@ -263,3 +263,18 @@ def test_plain_statement_of_rows():
     values = plain.scale_value(np.arange(0xf8))
     assert np.allclose(np.abs(s - a / 6), np.abs(values[:, None, None] - a / 6).min(0), rtol=1e-6)
     assert plain.nearest_scale(np.array([0.0, 1e9, 61440.0])).tolist() == [0, 0xe2, 0xe2] and plain.scale_value(0xe2) == 10240
+
+
+def test_list_workspace_is_bounded():
+    """The copy that the tensor-core form makes of a list takes 552 bytes an entry (d = 128) or 296: up to 8 GiB; longer lists take
+    the other form, whose workspace does not grow with them."""
+    most = 8 << 30
+    for d in (128, 64):
+        copied = []
+        for batch, n_kv in [(1, 1024), (8, 16384), (64, 1 << 20), (64, 1 << 22), (1, 1 << 26), (64, 1 << 25)]:
+            p = _cache(batch=batch, q_heads=8, kv_heads=8, d=d, n_kv=n_kv, n_q=8192, max_pages=1 << 20)
+            need = binding.cache4_attend_workspace_bytes(p, True)
+            assert need <= most, (d, batch, n_kv, need)
+            p.dtype = 0                                       # (fp32 queries: always the other form)
+            copied.append(need != binding.cache4_attend_workspace_bytes(p, True))
+        assert copied == [True, True, False, False, False, False]
