@@ -38,7 +38,7 @@ inline bool rope_turns(const double *inv_freq, int pairs, RopeTurns &out)
 __device__ __forceinline__ float2 rope_cos_sin(int64_t position, uint64_t turn, double scale, double sin_scale)
 {
     const int64_t frac = (int64_t)((uint64_t)position * turn);             // in [-1/2, 1/2) turns, 64 bits
-    const int quarter = (int)((frac + ((int64_t)1 << 61)) >> 62);
+    const int quarter = (int)((int64_t)((uint64_t)frac + (1ull << 61)) >> 62);       // (of 3/8 turns and more: -2)
     const int64_t rest = (int64_t)((uint64_t)frac - ((uint64_t)(int64_t)quarter << 62));
     const double x = (double)rest * (6.283185307179586476925286766559 * 0x1p-64), z = x * x;
     double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;         // 1 / 15!, 1 / 16!

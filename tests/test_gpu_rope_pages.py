@@ -283,3 +283,21 @@ def test_plan_of_as_many_places_as_there_can_be():
     assert got.slots[4:6004].tolist() == [table[i // 16] * 16 + i % 16 for i in range(6000)]
     for x in (got.positions, got.slots):
         assert all(bool((part == -1).all()) for part in x[6004:].split(1 << 28))
+
+
+@pytest.mark.parametrize("eighth", range(8))
+def test_angles_next_to_the_eighths_of_a_turn(eighth):
+    """Positions of a frequency of 2 pi / 4096: the angle's nearest quarter changes at its eighths, and at half a turn the fraction's sign does."""
+    rope = elm.Rope(64)
+    rope._freq[:] = [2 * np.pi / 4096] * 32
+    x = torch.randn(1, 1, 9, 64, generator=torch.Generator().manual_seed(3)).cuda()
+    for turns in (0, 1, -3, 1 << 40):
+        got = elm.rope(x, 4096 * turns + 512 * eighth - 4, rope)
+        # (the frequency is a double off by 2^-53 of itself, and so is an angle)
+        pos = np.arange(9) + 512 * eighth - 4
+        freq = np.array([2 * np.pi / 4096] * 32)
+        ref = plain.rotate(x.double().cpu().numpy(), pos, freq)
+        a = np.abs(x.double().cpu().numpy())
+        size = np.concatenate([a[..., :32] + a[..., 32:]] * 2, -1)
+        off = 4 * 2.0 ** -24 + abs(turns) * 2 * np.pi * 2.0 ** -53
+        assert (np.abs(got.double().cpu().numpy() - ref) <= off * size + 2.0 ** -24 * np.abs(ref)).all(), turns
