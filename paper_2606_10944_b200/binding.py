@@ -526,9 +526,14 @@ class Rope:
 
 def rope(X, positions, rope: Rope, inverse=False, out=None):
     """elm_rope: X [B, H, n, d] (any strides, a head's numbers side by side) rotated by positions, an int32 tensor [B, n] or the first
-    position of every sequence; ``inverse``: rotated back (the gradient).  ``out``: X itself, or another tensor of its shape."""
+    position of every sequence; ``inverse``: rotated back (the gradient).  ``out``: X itself, or another tensor of its shape.  Where X requires
+    a gradient, the result has one (without ``out``)."""
     tensor = isinstance(positions, torch.Tensor)
     device = _device(X, out, positions if tensor else None)
+    if X.requires_grad and torch.is_grad_enabled():
+        if out is not None:
+            raise ElmError("out: X requires a gradient, which a given place for the result does not have")
+        return _Rotation.apply(X, positions, rope, inverse)
     if device != torch.cuda.current_device():
         with torch.cuda.device(device):
             return _rope_again(X, positions, rope, inverse, out)
@@ -570,6 +575,25 @@ def rope(X, positions, rope: Rope, inverse=False, out=None):
 
 def _rope_again(X, positions, turn, inverse, out):              # (where ``rope`` is the name of an argument)
     return rope(X, positions, turn, inverse, out)
+
+
+class _Rotation(torch.autograd.Function):
+    """The rotation is linear: its gradient is the transposed one, elm_rope's inverse, and that one's is the rotation again."""
+
+    @staticmethod
+    def forward(ctx, X, positions, turn, inverse):
+        ctx.turn, ctx.inverse, ctx.first = turn, inverse, None
+        if isinstance(positions, torch.Tensor):
+            ctx.save_for_backward(positions)                    # (a later change of theirs is noticed)
+        else:
+            ctx.first = positions
+        return rope(X.detach(), positions, turn, inverse)
+
+    @staticmethod
+    def backward(ctx, dY):
+        if dY.stride(-1) != 1:
+            dY = dY.contiguous()
+        return rope(dY, ctx.saved_tensors[0] if ctx.first is None else ctx.first, ctx.turn, not ctx.inverse), None, None, None
 
 
 class PagePlan:

@@ -301,3 +301,75 @@ def test_angles_next_to_the_eighths_of_a_turn(eighth):
         size = np.concatenate([a[..., :32] + a[..., 32:]] * 2, -1)
         off = 4 * 2.0 ** -24 + abs(turns) * 2 * np.pi * 2.0 ** -53
         assert (np.abs(got.double().cpu().numpy() - ref) <= off * size + 2.0 ** -24 * np.abs(ref)).all(), turns
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_gradient_by_autograd(dtype, layout, inverse):
+    """Where X requires a gradient the result has it: the transposed rotation of the incoming one, against the 64-bit statement and
+    against differences; through strided, broadcast and other-stream uses, and again through itself."""
+    rope = elm.Rope(96, layout=layout, scaling="ramp", factor=4.0, original=1000)
+    g = torch.Generator().manual_seed(11)
+    wide = torch.randn(2, 13, 7, 128, generator=g).to(DTYPES[dtype]).cuda().requires_grad_()
+    x = wide[:, :, 1:5].transpose(1, 2)
+    pos = torch.randint(0, 5000, (2, 13), generator=g, dtype=torch.int32).cuda()
+    y = elm.rope(x, pos, rope, inverse=inverse)
+    with torch.no_grad():
+        assert torch.equal(y, elm.rope(x, pos, rope, inverse=inverse))
+    assert y.requires_grad
+    dy = torch.randn(y.shape, generator=g).to(DTYPES[dtype]).cuda()
+    got, = torch.autograd.grad(y, wide, dy, retain_graph=True)
+    assert (got[:, :, :1] == 0).all() and (got[:, :, 5:] == 0).all()
+    _check_rotation(got[:, :, 1:5].transpose(1, 2), dy, pos.cpu().numpy()[:, None], rope, layout, not inverse, wide.dtype)
+    # an incoming gradient that is one number, one with the numbers of a head apart, and one taken on another stream
+    one, = torch.autograd.grad(y.sum(), wide, retain_graph=True)
+    ref, = torch.autograd.grad(y, wide, torch.ones_like(y), retain_graph=True)
+    assert torch.equal(one, ref)
+    apart, = torch.autograd.grad(y, wide, dy.transpose(2, 3).contiguous().transpose(2, 3), retain_graph=True)
+    assert torch.equal(apart, got)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        other, = torch.autograd.grad(elm.rope(x, pos, rope, inverse=inverse), wide, dy)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(other, got)
+    # the gradient's own gradient is the rotation
+    v = dy.clone().requires_grad_()
+    back, = torch.autograd.grad(y, wide, v, create_graph=True)
+    u = torch.randn(wide.shape, generator=g).to(DTYPES[dtype]).cuda()
+    again, = torch.autograd.grad(back, v, u)
+    with torch.no_grad():
+        assert torch.equal(again, elm.rope(u[:, :, 1:5].transpose(1, 2), pos, rope, inverse=inverse))
+
+
+def test_gradient_against_differences():
+    rope = elm.Rope(64, scaling="ramp", factor=4.0, original=1000)
+    g = torch.Generator().manual_seed(12)
+    x = torch.randn(1, 2, 9, 64, generator=g).cuda().requires_grad_()
+    weight, step = torch.randn(1, 2, 9, 64, generator=g).cuda(), torch.randn(1, 2, 9, 64, generator=g).cuda()
+    value = lambda z: (elm.rope(z, 40, rope).double() * weight.double()).sum()      # noqa: E731
+    grad, = torch.autograd.grad(value(x), x)
+    h = 2.0 ** -4
+    with torch.no_grad():
+        diff = (value(x + h * step) - value(x - h * step)).item() / (2 * h)
+        # linear: each number of a rotation is off by 4 half steps of (|a| + |b|) scale, x +- h step by one more; so is the gradient's
+        size = rope.scale * 2 * weight.abs().max().item()
+        tol = 1152 * size * (2 * 5 * 2.0 ** -24 * (x.abs().max() + h * step.abs().max()).item() / (2 * h) + 4 * 2.0 ** -24 * step.abs().max().item())
+        assert abs((grad.double() * step.double()).sum().item() - diff) <= tol
+
+
+def test_gradient_refused_and_kept_apart():
+    rope = elm.Rope(64)
+    x = torch.randn(1, 2, 5, 64, generator=torch.Generator().manual_seed(1)).cuda().requires_grad_()
+    with pytest.raises(elm.ElmError):                         # a given place for the result has no gradient
+        elm.rope(x, 3, rope, out=torch.empty_like(x))
+    with torch.no_grad():
+        out = torch.empty_like(x)
+        assert torch.equal(elm.rope(x, 3, rope, out=out), elm.rope(x, 3, rope)) and not elm.rope(x, 3, rope).requires_grad
+    # positions that were changed between the two directions are noticed
+    pos = torch.arange(5, dtype=torch.int32)[None].cuda()
+    y = elm.rope(x, pos, rope)
+    pos += 1
+    with pytest.raises(RuntimeError):
+        y.sum().backward()
