@@ -877,8 +877,10 @@ def cache4_attend(Q, rows, table, length=None, idx=None, w=None, cu=None, max_q=
 def cache4_attend_status(workspace, params: Cache4Params, with_list: bool) -> int:
     """elm_cache4_attend_status: 0 unless a bounded device wait expired during the last cache4_attend call with this workspace."""
     out = ctypes.c_int32(-1)
-    _check(load_library().elm_cache4_attend_status(workspace.data_ptr(), ctypes.byref(params), int(with_list), ctypes.byref(out), _stream()),
-           "elm_cache4_attend_status")
+    device = _device(workspace)
+    with torch.cuda.device(device):
+        _check(load_library().elm_cache4_attend_status(workspace.data_ptr(), ctypes.byref(params), int(with_list), ctypes.byref(out),
+                                                       _stream_of(device)), "elm_cache4_attend_status")
     return int(out.value)
 
 

@@ -278,3 +278,42 @@ def test_list_workspace_is_bounded():
             p.dtype = 0                                       # (fp32 queries: always the other form)
             copied.append(need != binding.cache4_attend_workspace_bytes(p, True))
         assert copied == [True, True, False, False, False, False]
+
+
+def test_status_is_asked_on_the_workspaces_device(monkeypatch):
+    """cache4_attend_status runs on the device that its workspace is on and on that device's stream, whatever the current device is
+    (a library that notes what it is given stands in for two GPUs)."""
+    seen, entered = [], []
+
+    class Lib:
+        def elm_cache4_attend_status(self, workspace, params, with_list, out, stream):
+            seen.append((workspace, with_list, stream, list(entered)))
+            out._obj.value = 7
+            return 0
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            entered.append(self.index)
+
+        def __exit__(self, *_):
+            entered.pop()
+
+    class Workspace:
+        def get_device(self):
+            return 1
+
+        def data_ptr(self):
+            return 4096
+
+    monkeypatch.setattr(binding, "load_library", Lib)
+    monkeypatch.setattr(binding, "_stream_of", lambda device: 1000 + device)
+    monkeypatch.setattr(binding, "_stream", lambda: 1000)
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    assert binding.cache4_attend_status(Workspace(), _cache(n_kv=5), True) == 7
+    assert seen == [(4096, 1, 1001, [1])]
+    with pytest.raises(binding.ElmError):
+        monkeypatch.undo()
+        binding.cache4_attend_status(torch.zeros(16, dtype=torch.uint8), _cache(n_kv=5), True)      # not on a GPU
