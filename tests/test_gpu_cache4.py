@@ -715,3 +715,100 @@ def test_attend_tokens_cut_off(dtype, held, max_q):
                     ref = plain.attend(_np(Q[t, h * rep:(h + 1) * rep]), k, v, np.broadcast_to(np.arange(n) < upto, (rep, n)))
                     _check(out[t, h * rep:(h + 1) * rep], *ref, Q.dtype, n, (b, h, j))
         assert (out[torch.as_tensor(~written)] == 5.0).all()
+
+
+# ------------------------------------------------------------------------------------------------
+# forms that the calls above do not meet
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("n_core", [130, 2100])               # one CTA or a cluster, clusters
+@pytest.mark.parametrize("hidden", [(0, 32), (0, 64), (32, 64), (31, 129), (0, 129), (64, 2100)])
+def test_attend_list_tiles_not_seen(dtype, d, n_core, hidden):
+    """Whole tiles of 32 entries that are not seen: by weight, by number, by page, the first, the last and all but one among them."""
+    r = np.random.default_rng(n_core + hidden[1])
+    B, H, rep, page, n = 2, 2, 4, 32, 1500
+    table, n_pages = _tables(r, [n] * B, page, 50)
+    pool = _pool(r, n_pages, H, page, d)
+    idx, w = _list(r, B, H, n, n_core)
+    a, e = hidden[0], min(hidden[1], n_core)
+    table[1, 2] = -1
+    idx[1, 1][idx[1, 1] // page == 2] = 5
+    w[0, 0, a:e], w[0, 1, a:e] = 0.0, np.nan
+    idx[1, 0, a:e], idx[1, 1, a:e] = -5, 2 * page + 3
+    Q = torch.randn(B, H * rep, 1, d, generator=torch.Generator().manual_seed(2)).to(DTYPES[dtype]).cuda()
+    got = elm.cache4_attend(Q, pool, _ints(table), idx=_ints(idx), w=torch.as_tensor(w, dtype=torch.float32).cuda())
+    _check_list(pool, table, idx, w, Q, got, page, d)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_attend_list_of_many_queries_in_place_and_status(d):
+    """The tensor-core form over its own queries, and its status: 0, or what a bounded wait left that ran out (made to by a test hook; the
+    launch ends by itself), and 0 again after the next call."""
+    from paper_2606_10944_b200 import binding
+    lib = binding.load_library()
+    r = np.random.default_rng(d)
+    H, rep, page, n, n_core, n_q = 2, 2, 64, 900, 300, 3001
+    table, n_pages = _tables(r, [n], page, 16)
+    pool = _pool(r, n_pages, H, page, d)
+    idx, w = _list(r, 1, H, n, n_core)
+    Q = torch.randn(1, H * rep, n_q, d, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    assert _by_tensor_cores(Q, pool, table, n_core)
+    p = elm.Cache4Params(1, H * rep, H, d, 1, page, n_pages, 16, n_core, n_q)
+    ws = torch.empty(elm.cache4_attend_workspace_bytes(p, True), dtype=torch.uint8, device="cuda")
+    args = dict(idx=_ints(idx), w=torch.as_tensor(w, dtype=torch.float32).cuda(), workspace=ws)
+    t = _ints(table)
+    ref = elm.cache4_attend(Q, pool, t, **args)
+    assert elm.cache4_attend_status(ws, p, True) == 0
+    try:
+        assert lib.elm_debug_set(0, 20_000_000) == 0          # waits give up after 20 ms
+        assert lib.elm_debug_set(1, 1) == 0                   # the next launch misses one arrival per barrier
+        elm.cache4_attend(Q, pool, t, **args)
+        torch.cuda.synchronize()
+        assert elm.cache4_attend_status(ws, p, True) != 0
+    finally:
+        assert lib.elm_debug_set(0, 2_000_000_000) == 0
+    assert elm.cache4_attend(Q, pool, t, out=Q, **args) is Q
+    assert elm.cache4_attend_status(ws, p, True) == 0 and torch.equal(Q, ref)
+    p = elm.Cache4Params(1, H * rep, H, d, 1, page, n_pages, 16, 0, 1)
+    ws = torch.empty(elm.cache4_attend_workspace_bytes(p, False), dtype=torch.uint8, device="cuda")
+    elm.cache4_attend(Q[:, :, :1].contiguous(), pool, t, length=_ints([n]), workspace=ws)
+    assert elm.cache4_attend_status(ws, p, False) == 0
+
+
+def test_threads_that_share_a_rotation():
+    """Steps of many sizes from two threads on streams of their own, with one Rope: what each does alone."""
+    import threading
+    d, H, page = 128, 2, 16
+    rope = elm.Rope(d)
+    sizes = list(range(1, 41))
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(40, H, d, generator=g).cuda()
+    table, length = _ints(np.arange(4)[None]), _ints([40])
+
+    def steps(rope):
+        rows = elm.cache4_pool(4, H, page, d)
+        rows.zero_()
+        for n in sizes:
+            k = x[:n]
+            q = elm.cache4_append(rows, k, k, _ints(np.arange(n)), rope=rope, positions=_ints(np.arange(n)), Q=k)
+            y = elm.rope(k[None].transpose(1, 2), 5, rope)
+        o = elm.cache4_attend(q.transpose(0, 1)[None].contiguous(), rows, table, length=length)
+        return rows, q, y, o
+
+    want = steps(elm.Rope(d))
+    torch.cuda.synchronize()
+    found = {}
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            found[i] = steps(rope)
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for i in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(found[i], want))
