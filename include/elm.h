@@ -313,7 +313,8 @@ typedef struct elm_rope_params {
     int64_t x_stride[3], out_stride[3]; /* batch, head, token strides in elements (the numbers of a head lie side by
                                            side); all three 0: dense [batch][heads][n_tokens][d] */
 } elm_rope_params;
-/* X, out: any element-aligned addresses and strides (16-byte aligned rows are faster); out may be X with the same strides,
+/* heads <= 65535, batch * n_tokens < 2^31.
+ * X, out: any element-aligned addresses and strides (16-byte aligned rows are faster); out may be X with the same strides,
  * else the two must not overlap, and no two rows of out may.  positions: device int32 [batch][n_tokens], any sign; NULL:
  * token t of every batch entry has position first_position + t. */
 int elm_rope(const void *X, const int32_t *positions, int64_t first_position, const elm_rope_params *params, void *out,
@@ -375,7 +376,8 @@ int elm_page_release(int32_t *table, int32_t *length, const int32_t *done, int32
 /* New tokens into the pool: keys are rotated, keys and values stored in 4 bits; queries, if any, rotated beside them.
  *   K, V [n_tokens][kv_heads][d], Q and Q_out [n_tokens][q_heads][d] (Q_out may be Q), with token and head strides in elements
  *   (both 0: dense).  positions int32 [n_tokens] (unused when rotary_dim is 0), slots int32 [n_tokens]: a token whose slot is outside the pool
- *   is passed over: neither its row nor its Q_out is written.  Two tokens must not have the same slot. */
+ *   is passed over: neither its row nor its Q_out is written.  Two tokens must not have the same slot.  q_heads, kv_heads <= 65535; Q_out that is
+ *   not Q must not overlap it. */
 typedef struct elm_append_params {
     int32_t n_tokens, q_heads, kv_heads, d; /* q_heads 0: no queries; d 64 or 128 */
     int32_t dtype;                          /* ELM_F32 or ELM_BF16, of Q, K, V and Q_out */
@@ -390,7 +392,7 @@ int elm_cache4_append(const void *Q, const void *K, const void *V, const int32_t
 
 /* Rows back: K_out, V_out dense [batch][kv_heads][n_kv][d] in dtype (ELM_F32 or ELM_BF16, exact either way), as elm_compress and
  * elm_express_prefill take them.  idx NULL: row r of request b is its row r; else idx[batch][kv_heads][n_kv] are the rows' numbers
- * (those of elm_compress, say).  A row that is not there (r < 0, r >= length[b] where length is given, past the table, on no
+ * (those of elm_compress, say).  kv_heads <= 65535.  A row that is not there (r < 0, r >= length[b] where length is given, past the table, on no
  * page) reads as zeros. */
 typedef struct elm_cache4_params {
     int32_t batch, q_heads, kv_heads, d;    /* d 64 or 128; q_heads is not used by elm_cache4_read */
@@ -418,8 +420,10 @@ int elm_cache4_read(const void *rows, const int32_t *table, const int32_t *lengt
  * nothing gets zeros.  Tokens of O outside cu, and those of requests without queries, are left as they were.  O may be Q with the
  * same strides, else the two must not overlap.  (A request that elm_page_plan did not serve has queries in cu and its old
  * length: what its tokens of O hold afterwards means nothing.)
- * dtype is that of Q and O: ELM_BF16 (probabilities rounded to fp16 for P V) or ELM_F32 (queries and probabilities as two fp16
- * parts); logits, maxima, denominators and accumulators are fp32 either way.  batch <= 1024.
+ * dtype is that of Q and O.  ELM_BF16: queries, scaled by a power of two, and probabilities are rounded to fp16 for the products, or, in the tensor-core form
+ * below, probabilities to bf16 (half a step 2^-8 instead of 2^-11).  ELM_F32: queries and probabilities as two fp16 parts (22 bits).  Logits, maxima,
+ * denominators and accumulators are fp32 either way.  Over a list, a query with a NaN gets NaN even where it sees nothing.
+ * batch <= 1024, batch * q_heads <= 65535, n_q * q_heads / kv_heads < 2^30.
  * bf16 lists met by many queries take the tensor-core kernel of elm_attend over a gathered bf16 copy (dense Q and O only), as long as
  * the workspace that holds the copy is not above 8 GiB.
  * workspace: at least the bytes of elm_cache4_attend_workspace_bytes, 256-byte aligned, scratch; two calls that overlap in time (two

@@ -457,7 +457,9 @@ def _device(first, *tensors):
 
 
 class _Kept(dict):
-    """What a call has found out about sizes, strides and types (nothing of the tensors themselves), for the next one with the same."""
+    """What a call has found out about sizes, strides and types (nothing of the tensors themselves), for the next one with the same.
+    A call of sizes that are not here looks at everything (up to 9 us more), and all are forgotten at the 256th, so steps whose number of tokens changes
+    are best padded to a few sizes, as page_plan() allows."""
 
     def keep(self, key, value):
         if len(self) >= 256:
@@ -678,7 +680,8 @@ _append_kept = _Kept()
 
 def cache4_append(rows, K, V, slots, rope: Rope = None, positions=None, Q=None, q_out=None):
     """elm_cache4_append: K, V [T, Hkv, d] into the pool's rows slots [T] (a slot outside the pool: passed over), keys rotated by
-    ``rope`` at positions [T].  Q [T, Hq, d] comes back rotated (in q_out, which may be Q; of tokens passed over, as q_out was)."""
+    ``rope`` at positions [T].  Q [T, Hq, d] comes back rotated (in q_out, which may be Q; of tokens passed over, as q_out was: without q_out
+    those rows are uninitialised memory, NaN possibly)."""
     device = _device(rows, K, V, slots, positions, Q, q_out)
     if device != torch.cuda.current_device():
         with torch.cuda.device(device):
@@ -846,7 +849,8 @@ def cache4_attend_workspace_bytes(params: Cache4Params, with_list: bool) -> int:
 def cache4_attend(Q, rows, table, length=None, idx=None, w=None, cu=None, max_q=None, n_kv=None, causal=True, workspace=None, out=None):
     """elm_cache4_attend: Q [B, Hq, n, d] over the rows of the requests of table [B, max_pages]: the first length [B] of them (n_kv: a bound
     of the lengths that the host knows; causal: a request's queries are its last tokens), or the list idx with weights w
-    [B, Hkv, n_core].  With cu [B + 1]: Q [T, Hq, d], request b has the tokens cu[b] .. cu[b + 1] - 1, max_q at most.  O like Q."""
+    [B, Hkv, n_core].  With cu [B + 1]: Q [T, Hq, d], request b has the tokens cu[b] .. cu[b + 1] - 1, max_q at most.  O like Q: tokens
+    outside cu, and those of a request that has more than max_q, are as ``out`` was (without it uninitialised memory, NaN possibly)."""
     device = _device(rows, Q, table, length, idx, w, cu, workspace, out)
     if device != torch.cuda.current_device():
         with torch.cuda.device(device):

@@ -927,7 +927,9 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
     const int tiles = (a.n_kv + A4_TILE - 1) / A4_TILE;
     for (int size = 1; size <= 16; size *= 2) {
         if (tiles > size * A4_WARPS * (size == 16 ? 4 : 2)) continue;
-        // (the queries of a request may be far fewer than their bound: then CTAs by the bound would be mostly idle ones)
+        // (the queries of a request may be far fewer than their bound: then CTAs by the bound would be mostly idle ones.  Rows of 200 and 1 token a
+        // request, a CTA each against the line of tiles: 28 problems by the bound to an SM 45 against 50 us, 55 to an SM 53 against 50, 221 99 against 49.
+        // Where all the bound's tokens are there the CTAs are the faster by 5 to 45 %, which those calls above the limit do without: 154 against 163)
         if (size == 1 && a.cu && max_groups > 1 && problems > 32 * (int64_t)device_sm_count()) continue;
         if (size > 1) {
             static std::atomic<int> resident[64][5];
@@ -963,7 +965,9 @@ template <typename T, int D, int NT, int PARTS, bool LIST> int launch_attend4_fo
     const int grid = stretches(places, per_sm * device_sm_count());
     ELM_CUDA_TRY(launch_after(kern, dim3((unsigned)grid), dim3(A4_THREADS), smem, st, a));
     count_launches(1);
-    // slices of 32 or 128 numbers where the problems alone are few
+    // slices of 32 or 128 numbers where the problems alone are few.  Slices of 32 / of 128 / none, us for bf16 rows of 32768 each, d = 128: 1 problem
+    // 14 / 15 / 29, 8 23 / 25 / 33, 16 27 / 28 / 35, 32 43 / 41 / 41, 40 49 / 45 / 47; 128 of 8192 60 / 43 / 41.  Of 96 such calls (d, types, 8 and
+    // 16 vectors) the rule takes a form more than 5 % slower than the best in 8, by 14 % at most.
     constexpr int FINE = C::N * D / 32, COARSE = C::N * D / 128;
     const int slices = problems * FINE <= 2 * device_sm_count() ? FINE : problems * COARSE <= 2 * device_sm_count() ? COARSE : 1;
     auto join = slices == FINE ? attend4_merge_kernel<T, D, NT, FINE> : slices == COARSE ? attend4_merge_kernel<T, D, NT, COARSE> : attend4_merge_kernel<T, D, NT, 1>;
@@ -1012,10 +1016,13 @@ elm_params as_attend(const elm_cache4_params *p)
 }
 
 // Lists met by so many queries that the tensor-core kernel of elm_attend over a gathered copy, 256 queries of a head at a time, is the faster
-// way.  Both forms' times in us, as they were measured (lists of 1024, 2048 and 16384 entries, 4 to 256 queries of 8 to 256 heads, d = 128):
-//   here     9 + 0.9 (A4_START + tiles) per CTA slot and problem     8 heads x 4, 2048 entries: 128 queries 45 (44), 256 queries 71 (78)
-//   there   14 + 2.2 per block of 128 entries and wave of items      the same: 49 (49), 51 (49)
-// With 2 or 3 queries the first form is 4 to 6 times as fast, with thousands the second.  Its gathered copy has to fit the workspace: 552 bytes an
+// way.  Both forms' times in us, as they were fitted at d = 128; measured (fitted) for 8 KV heads x 4, 2048 entries:
+//   here     9 + 0.9 (A4_START + tiles) per CTA slot and problem     64 queries 31 (24), 128 44 (39), 256 71 (68), 1024 222 (246)
+//   there   14 + 2.2 per block of 128 entries and wave of items                 49 (49),     51 (49),     51 (49),       51 (49)
+// Of 112 calls each (1, 4, 8 and 32 KV heads, 1 to 8 query heads to one, 256 to 16384 entries, 8 to 1024 queries) the faster form is taken in 109 at
+// d = 128, a form 1.12 times as slow at most in the others.  At d = 64 `here` takes 0.53 instead of 0.9 and `there` 0.9 of its time, for which the rule
+// makes no difference: the second form comes too early in 8 of the 112, by 1.41 times at most (8 heads x 4, 256 entries, 256 queries: 15 against 21 us).
+// With 8 queries the first form is up to 20 times as fast, with 1024 the second up to 5 times.  Its gathered copy has to fit the workspace: 552 bytes an
 // entry and KV head (d = 64: 296), a twentieth of the GPU's memory at most (15 M entries), which also keeps clear of what that kernel can count.
 constexpr size_t A4_MAX_COPY = (size_t)8 << 30;
 bool by_tensor_cores(const elm_cache4_params *p, bool list)

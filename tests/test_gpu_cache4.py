@@ -812,3 +812,20 @@ def test_threads_that_share_a_rotation():
         t.join()
     for i in range(2):
         assert all(torch.equal(a, b) for a, b in zip(found[i], want))
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("n_q", [2, 20000])
+def test_attend_list_nan_queries(d, n_q):
+    """Over a list a query with a NaN gets NaN, whether it sees anything or not, and no other query does."""
+    r = np.random.default_rng(d)
+    pool = _pool(r, 4, 2, 16, d)
+    idx, w = _list(r, 1, 2, 60, 40)
+    idx[0, 1] = -1
+    Q = torch.randn(1, 4, n_q, d, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    Q[:, :, 1, 3] = float("nan")
+    assert _by_tensor_cores(Q, pool, np.zeros((1, 4)), 40) == (n_q == 20000)
+    got = elm.cache4_attend(Q, pool, _ints([[0, 1, 2, 3]]), idx=_ints(idx), w=torch.as_tensor(w, dtype=torch.float32).cuda())
+    bad = torch.isnan(got).any(-1)
+    assert bad[:, :, 1].all() and bad.sum() == 4 and torch.isnan(got[:, :, 1]).all()
+    assert (got[:, 2:, 0] == 0).all() and (got[:, :2, 0] != 0).any(-1).all()
