@@ -829,3 +829,24 @@ def test_attend_list_nan_queries(d, n_q):
     bad = torch.isnan(got).any(-1)
     assert bad[:, :, 1].all() and bad.sum() == 4 and torch.isnan(got[:, :, 1]).all()
     assert (got[:, 2:, 0] == 0).all() and (got[:, :2, 0] != 0).any(-1).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rep", [1, 3])
+def test_attend_prompt_chunks(dtype, rep):
+    """Hundreds of new tokens to a request, behind rows that were there and at its beginning; some of the tokens against 64 bits."""
+    r = np.random.default_rng(rep)
+    d, H, page = 64, 2, 32
+    lengths, new = [2900, 701, 1, 40], [513, 701, 1, 39]
+    table, n_pages = _tables(r, lengths, page, 100)
+    pool = _pool(r, n_pages, H, page, d)
+    cu = np.concatenate([[0], np.cumsum(new)])
+    Q = torch.randn(cu[-1], H * rep, d, generator=torch.Generator().manual_seed(1)).to(DTYPES[dtype]).cuda()
+    got = elm.cache4_attend(Q, pool, _ints(table), length=_ints(lengths), cu=_ints(cu), max_q=max(new))
+    for b, n in enumerate(lengths):
+        k, v = zip(*[_rows_of(pool, table, b, h, np.arange(n), page, d) for h in range(H)])
+        for j in sorted({0, 1, 31, 32, new[b] // 2, new[b] - 2, new[b] - 1} & set(range(new[b]))):
+            t, upto = cu[b] + j, n - new[b] + 1 + j
+            for h in range(H):
+                ref = plain.attend(_np(Q[t, h * rep:(h + 1) * rep]), k[h], v[h], np.broadcast_to(np.arange(n) < upto, (rep, n)))
+                _check(got[t, h * rep:(h + 1) * rep], *ref, Q.dtype, n, (b, h, j))

@@ -373,3 +373,24 @@ def test_gradient_refused_and_kept_apart():
     pos += 1
     with pytest.raises(RuntimeError):
         y.sum().backward()
+
+
+def test_gradient_captured():
+    """Both directions in one graph, replayed over other numbers."""
+    rope = elm.Rope(64)
+    g = torch.Generator().manual_seed(2)
+    x = torch.randn(1, 2, 9, 64, generator=g).cuda().requires_grad_()
+    dy = torch.randn(1, 2, 9, 64, generator=g).cuda()
+    pos = torch.arange(9, dtype=torch.int32)[None].cuda()
+    torch.autograd.grad(elm.rope(x, pos, rope), x, dy)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = elm.rope(x, pos, rope)
+        dx, = torch.autograd.grad(y, x, dy)
+    with torch.no_grad():
+        x.copy_(torch.randn(x.shape, generator=g))
+    dy.copy_(torch.randn(x.shape, generator=g))
+    graph.replay()
+    torch.cuda.synchronize()
+    with torch.no_grad():
+        assert torch.equal(y, elm.rope(x, pos, rope)) and torch.equal(dx, elm.rope(dy, pos, rope, inverse=True))
